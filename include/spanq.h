@@ -452,6 +452,129 @@ int span_model_forward(span_model* model, span_plan_t* plan, const int32_t* row_
 int span_model_decode(span_model* model, span_plan_t* plan, const int32_t* tokens, float* logits_out,
                       int32_t* next_tokens, void* stream);
 
+/* ---------------------------------------------------------------- row operators */
+
+/* Steps of a decoder stack over rows of many requests, for callers that run their own
+ * layers around the attention calls; span_model_* calls them too.  Common to all:
+ * - memory is the caller's, on `device`; a call is enqueued on `stream` (a stream of that
+ *   device) and returns.  Nothing is allocated, nothing waits, and no call keeps anything
+ *   for the next: a call may be captured into a graph, and calls with workspaces of their
+ *   own may overlap.  The device that was current stays so.
+ * - strides are in elements, from row to row; inside a row elements follow one another.
+ * - device arrays of indices are read by the kernels: an index outside its range is
+ *   answered as each operator says, never followed.
+ * - outputs overlap no input, but for the same row in place where an operator says so.
+ * - no rows is SPAN_OK without a launch.  SPAN_EINVAL on a bad argument. */
+
+/* Norms of queries and keys for each head, their rotation in the same pass, and the rows'
+ * way from one q|k|v product to the caller's rows:
+ *     y = x / sqrt(mean(x^2) + eps) * gain      over the head_dim values of a head
+ *     then rotated by positions[i] * rope_theta^(-2j/d) (rotate-half pairs j, j + d/2)
+ * Values are copied.  span_prefill_fragments, span_cross_attend and span_decode_attend
+ * rotate by themselves: give them rows made with positions = NULL.
+ * In place: an output equal to its input, with the same stride and rows = NULL. */
+typedef struct {
+  const void* q;      /* [n_rows][num_q_heads][head_dim]; any of q, k, v may be NULL with its output */
+  const void* k;      /* [n_rows][num_kv_heads][head_dim] */
+  const void* v;
+  void* q_out;        /* [out_rows][num_q_heads][head_dim] */
+  void* k_out;        /* [out_rows][num_kv_heads][head_dim] */
+  void* v_out;
+  const void* q_gain; /* [head_dim], NULL: queries are not normed */
+  const void* k_gain;
+  const int32_t* rows;      /* device [n_rows]: the output row of each row, NULL: its own index.  A row
+                               outside [0, out_rows) is not written; output rows that none names stay
+                               as they are; two rows that name the same one are an error not found */
+  const int32_t* positions; /* device [n_rows], NULL: no rotation */
+  int64_t q_stride, k_stride, v_stride;             /* of the inputs; multiples of 16 bytes */
+  int64_t q_out_stride, k_out_stride, v_out_stride; /* of the outputs */
+  int64_t n_rows;     /* below 2^31 */
+  int64_t out_rows;   /* at least n_rows when rows is NULL */
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t dtype;      /* SPAN_F32 or SPAN_BF16: rows and gains */
+  int32_t device;
+  float eps;          /* >= 0 */
+  float rope_theta;   /* > 0 */
+  int32_t reserved;   /* 0 */
+} span_qk_norm;
+int span_qk_norm_rope(const span_qk_norm* args, void* stream);
+
+/* Low-rank adapters of many requests at once beside a shared projection:
+ *     out[i] = base[i] + scale[a] * (x[i] A[a]^T) B[a]^T,   a = ids[i]
+ * bf16 rows and weights, sums in fp32, one rounding of the result.  A projection of several
+ * column parts (q|k|v, gate|up) has an A for each part and a B over all columns.  Rows
+ * come in any order; rows whose id lies outside [0, n_adapters) get base[i].
+ * In place: out == base with the same stride.  A row's result depends on its own x, base
+ * and adapter, and in its last bits on the number of rows of the call. */
+typedef struct {
+  const void* x;      /* [n_rows][in_features] */
+  const void* base;   /* [n_rows][out], out = the sum of part_cols: the projection's result */
+  void* out;          /* [n_rows][out] */
+  const int32_t* ids; /* device [n_rows] */
+  const void* a;      /* [n_adapters][n_parts][max_rank][in_features] */
+  const void* b;      /* [n_adapters][out][max_rank] */
+  const float* scale; /* device [n_adapters], NULL: 1 */
+  const int32_t* ranks; /* device [n_adapters], NULL: max_rank.  What lies past an adapter's rank
+                           does not count and may hold anything */
+  void* workspace;    /* span_adapter_workspace bytes, 16-byte aligned */
+  size_t workspace_bytes;
+  int64_t x_stride, base_stride, out_stride; /* multiples of 8; rows 16-byte aligned, as a and b */
+  int64_t n_rows;     /* below 2^31 */
+  int32_t in_features; /* multiple of 8, at most 2^20 */
+  int32_t n_adapters;
+  int32_t max_rank;   /* multiple of 8, 8 .. 128: smaller ranks are padded, with zeros or by `ranks` */
+  int32_t n_parts;    /* 1 .. 4 */
+  int32_t part_cols[4]; /* multiples of 8; all together at most 2^20 */
+  int32_t device;
+  int32_t reserved;   /* 0 */
+} span_adapter_call;
+/* Workspace of a call: from n_rows, in_features, max_rank and n_parts. */
+int span_adapter_workspace(const span_adapter_call* args, size_t* bytes);
+int span_adapter_apply(const span_adapter_call* args, void* stream);
+
+/* Verification of drafted tokens against the target's probabilities, from given random
+ * numbers, so that kept and drawn tokens are distributed as the target's own (speculative
+ * sampling); with max_drafts = 0, a token sampled for each request.  Request q's target
+ * rows are target_row0[q] .. + n_drafts[q], row j the logits after its first j drafts.
+ * With p_j the softmax of row j at temperature T and q_j the draft's (its logits' softmax at T,
+ * or 1 at the drafted token if draft_logits is NULL):
+ *     draft j with token d is kept if u_accept[q][j] q_j(d) < p_j(d) and all before it were;
+ *     then one more token: the first i whose running sum of w exceeds u_sample[q] times the whole,
+ *     w = max(p_a - q_a, 0) at the first refused draft a (p_a if that is nothing), p_n after the last.
+ * T <= 0 (or NaN): greedy; a draft is kept if it is its row's argmax, the token is the argmax.  The lowest
+ * id wins ties.  Logits of -inf and NaN have no weight, of +inf all of it.  Weights and sums
+ * are 64-bit.  A drafted id outside the vocabulary is refused.
+ * A request whose rows lie outside the logits gets accepted = -1; one whose deciding row has no
+ * weight at all gets the token -1. */
+#define SPAN_MAX_DRAFTS 64
+typedef struct {
+  const float* target_logits; /* [target_rows][vocab] */
+  const float* draft_logits;  /* [draft_rows][vocab], NULL: drafts without a distribution */
+  const int32_t* target_row0; /* device [n_requests], NULL: q (max_drafts + 1) */
+  const int32_t* draft_row0;  /* device [n_requests], NULL: q max_drafts */
+  const int32_t* drafts;      /* device [n_requests][max_drafts], NULL only with max_drafts = 0 */
+  const int32_t* n_drafts;    /* device [n_requests], NULL: max_drafts; taken into 0 .. max_drafts */
+  const float* u_accept;      /* device [n_requests][max_drafts], in [0, 1) */
+  const float* u_sample;      /* device [n_requests], in [0, 1) */
+  const float* temperature;   /* device [n_requests], NULL: 1 */
+  int32_t* accepted;          /* device [n_requests]: drafts kept */
+  int32_t* tokens;            /* device [n_requests][max_drafts + 1]: the kept drafts, the next token, then -1 */
+  float* logprobs;            /* device, as tokens, or NULL: log p of each token (at T = 1 if greedy), 0 past them */
+  void* workspace;            /* span_verify_workspace bytes, 16-byte aligned */
+  size_t workspace_bytes;
+  int64_t target_stride, draft_stride; /* at least vocab */
+  int64_t target_rows, draft_rows;
+  int32_t n_requests;         /* at most 2^20 */
+  int32_t max_drafts;         /* 0 .. SPAN_MAX_DRAFTS */
+  int32_t vocab;              /* 1 .. 2^24 */
+  int32_t device;
+} span_verify_call;
+/* Workspace of a call: from n_requests, max_drafts and vocab. */
+int span_verify_workspace(const span_verify_call* args, size_t* bytes);
+int span_verify_drafts(const span_verify_call* args, void* stream);
+
 /* ---------------------------------------------------------------- debug */
 
 /* Kernel durations of a plan's launches on a pool created with SPAN_FLAG_TIMING,

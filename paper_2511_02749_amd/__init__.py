@@ -22,3 +22,11 @@ from ._lib import (  # noqa: F401
     probe_mfma_peak,
     probe_read_peak,
 )
+from .row_ops import (  # noqa: F401
+    SPAN_MAX_DRAFTS,
+    adapter_apply,
+    adapter_workspace,
+    qk_norm_rope,
+    verify_drafts,
+    verify_workspace,
+)

@@ -31,7 +31,8 @@ EXPORTS = [
     "span_plan_commit", "span_plan_destroy", "span_plan_kernel_times", "span_probe_mfma_peak",
     "span_probe_read_peak", "span_plan_static", "span_model_create", "span_model_destroy", "span_model_forward",
     "span_parse_serialized", "span_bulk_order", "span_plan_moves", "span_plan_decode", "span_decode_attend",
-    "span_model_decode", "span_probe_gemm",
+    "span_model_decode", "span_probe_gemm", "span_qk_norm_rope", "span_adapter_workspace", "span_adapter_apply",
+    "span_verify_workspace", "span_verify_drafts",
 ]
 SPAN_STATIC_SCRATCH_BYTES = 64 << 20
 SPAN_FLAG_TIMING = 1
@@ -161,6 +162,12 @@ def load():
         "span_probe_mfma_peak": (I32, [I32, I32, VP, P(ctypes.c_double)]),
         "span_probe_read_peak": (I32, [VP, ctypes.c_size_t, I32, VP, P(ctypes.c_double)]),
         "span_probe_gemm": (I32, [VP, VP, VP, I64, I64, I64, I32, I32, VP, P(I32), P(ctypes.c_double)]),
+        # argument records packed by row_ops.py
+        "span_qk_norm_rope": (I32, [ctypes.c_char_p, VP]),
+        "span_adapter_workspace": (I32, [ctypes.c_char_p, P(ctypes.c_size_t)]),
+        "span_adapter_apply": (I32, [ctypes.c_char_p, VP]),
+        "span_verify_workspace": (I32, [ctypes.c_char_p, P(ctypes.c_size_t)]),
+        "span_verify_drafts": (I32, [ctypes.c_char_p, VP]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)

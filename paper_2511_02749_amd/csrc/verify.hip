@@ -8,7 +8,7 @@
 //   T <= 0: a draft is kept if it is the argmax of x_j, the next token is the argmax of x_a
 //
 // Three launches (two where no draft has a distribution):
-// 1. every row in chunks of kChunk logits, one work-group each: the chunk's largest logit, its
+// 1. every row in chunks of kChunk logits, one wave each: the chunk's largest logit, its
 //    lowest id, and the sum of exp against it;
 // 2. (draft logits) the chunks of the one row that decides a request: sums of max(p - q, 0);
 // 3. one work-group per request: the chunk where the running sum passes u, then the token in
@@ -18,8 +18,8 @@
 //
 // Weights and sums are 64-bit: borders of the running sum over 10^5 tokens lie 10^-5 and
 // less apart, where 32-bit sums, and their order, would choose another token every few
-// thousand calls.  64-bit instructions run at the 32-bit rate here; the exponential is its
-// Taylor series on [-ln 2 / 2, ln 2 / 2] to the 11th power (6e-15 relative).
+// thousand calls.  64-bit instructions run at the 32-bit rate here; the exponential is the
+// Taylor series of 2^f on [-1/2, 1/2] to the 11th power (6e-15 relative), without a branch.
 //
 // Bound: HBM, each logit read once (and the deciding row again, from the last-level cache),
 // about 20 vector instructions per logit beside it.
@@ -34,10 +34,12 @@ namespace spanq {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kChunk = 4096;
-constexpr int kPer = kChunk / kThreads;
-constexpr int kPickThreads = 1024;
+constexpr int kWaves = kThreads / 64;
+constexpr int kChunk = 2048;        // logits of a wave in 1 and 2: 63 chunks of 128256, one for each lane in 3
+constexpr int kPer = kChunk / 64;
+constexpr int kPickThreads = 1024;  // a wave for each row of up to seven drafts and their distributions
 constexpr int kMaxDrafts = SPAN_MAX_DRAFTS;
+constexpr double kLog2e = 1.4426950408889634074;
 
 struct Stat {
   double sum;  // of exp((x - max) / T) over the chunk
@@ -54,48 +56,99 @@ struct Args {
   double* left;    // [requests][chunks]: sums of max(p - q, 0)
 };
 
-// exp(t) for t <= 0; 0 below -700, and for a NaN.
-__device__ __forceinline__ double exp_neg(double t) {
-  if (!(t > -700.0)) return 0.0;
-  const double k = rint(t * 1.4426950408889634074);  // t = k ln 2 + f
-  const double f = fma(k, -0.69314718055994530942, t);
-  double p = 1.0 / 39916800.0;
-  p = fma(p, f, 1.0 / 3628800.0);
-  p = fma(p, f, 1.0 / 362880.0);
-  p = fma(p, f, 1.0 / 40320.0);
-  p = fma(p, f, 1.0 / 5040.0);
-  p = fma(p, f, 1.0 / 720.0);
-  p = fma(p, f, 1.0 / 120.0);
-  p = fma(p, f, 1.0 / 24.0);
-  p = fma(p, f, 1.0 / 6.0);
-  p = fma(p, f, 0.5);
-  p = fma(p, f, 1.0);
+// 2^t for t <= 0 (and up to 1); 0 for -inf and NaN, whose bound, 2^-1200, underflows.
+__device__ __forceinline__ double exp2_neg(double t) {
+  t = fmax(t, -1200.0);
+  const double k = rint(t), f = t - k;
+  // ln(2)^n / n!
+  double p = 4.4455382718708114976e-10;
+  p = fma(p, f, 7.0549116208011233299e-9);
+  p = fma(p, f, 1.0178086009239699728e-7);
+  p = fma(p, f, 1.3215486790144309488e-6);
+  p = fma(p, f, 1.5252733804059840280e-5);
+  p = fma(p, f, 1.5403530393381609954e-4);
+  p = fma(p, f, 1.3333558146428443423e-3);
+  p = fma(p, f, 9.6181291076284771620e-3);
+  p = fma(p, f, 5.5504108664821579953e-2);
+  p = fma(p, f, 2.4022650695910071233e-1);
+  p = fma(p, f, 6.9314718055994530942e-1);
   p = fma(p, f, 1.0);
   return ldexp(p, static_cast<int>(k));
 }
 
-// The weight of logit x against the largest one: 1 at it (an infinite one too), else
-// exp((x - max) / T); 0 for -inf and NaN.
-__device__ __forceinline__ double weight(float x, float max, double inv_t) {
-  if (!(max > -INFINITY)) return 0.0;
-  if (x == max) return 1.0;
-  return exp_neg((static_cast<double>(x) - static_cast<double>(max)) * inv_t);
+// The weight of logit x against the row's (or chunk's) largest one, c = log2(e) / T: 1 at it
+// (an infinite one too), else exp((x - max) / T); 0 for -inf and NaN.
+__device__ __forceinline__ double weight(float x, float max, double c) {
+  const double w = exp2_neg((static_cast<double>(x) - static_cast<double>(max)) * c);
+  return max > -INFINITY ? (x == max ? 1.0 : w) : 0.0;
 }
 
-__device__ __forceinline__ void better(float& bv, int& bi, float v, int i) {
-  if (v > bv || (v == bv && i < bi)) {
-    bv = v;
-    bi = i;
-  }
+// Values of other lanes by vector instructions alone: DPP rotations inside a row of 16, and
+// swaps of rows and of halves.
+template <int kCtrl, int kRows = 0xf>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+  return __builtin_amdgcn_update_dpp(0, v, kCtrl, kRows, 0xf, true);
 }
-
-__device__ __forceinline__ double shfl_xor_f64(double v, int off) { return __shfl_xor(v, off); }
+template <int kCtrl, int kRows = 0xf>
+__device__ __forceinline__ double dpp(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint64_t lo = dpp<kCtrl, kRows>(static_cast<uint32_t>(u));
+  const uint64_t hi = dpp<kCtrl, kRows>(static_cast<uint32_t>(u >> 32));
+  return __builtin_bit_cast(double, lo | hi << 32);
+}
+// v of all 64 lanes joined by f, which commutes: the same bits in every lane.
+template <class F>
+__device__ __forceinline__ uint32_t join32(uint32_t v, F f) {
+  v = f(v, dpp<0x128>(v));  // row_ror:8, 4, 2, 1
+  v = f(v, dpp<0x124>(v));
+  v = f(v, dpp<0x122>(v));
+  v = f(v, dpp<0x121>(v));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = f(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return f(b[0], b[1]);
+}
+__device__ __forceinline__ float wave_max(float v) {
+  return __uint_as_float(join32(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+__device__ __forceinline__ int wave_min(int v) {
+  return static_cast<int>(join32(static_cast<uint32_t>(v), [](uint32_t a, uint32_t b) {
+    return static_cast<uint32_t>(min(static_cast<int>(a), static_cast<int>(b)));
+  }));
+}
+__device__ __forceinline__ double wave_sum(double v) {
+  v += dpp<0x128>(v);
+  v += dpp<0x124>(v);
+  v += dpp<0x122>(v);
+  v += dpp<0x121>(v);
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  auto lo = __builtin_amdgcn_permlane16_swap(static_cast<uint32_t>(u), static_cast<uint32_t>(u), false, false);
+  auto hi = __builtin_amdgcn_permlane16_swap(static_cast<uint32_t>(u >> 32), static_cast<uint32_t>(u >> 32), false, false);
+  auto pair = [](uint32_t l, uint32_t h) { return __builtin_bit_cast(double, static_cast<uint64_t>(h) << 32 | l); };
+  v = pair(lo[0], hi[0]) + pair(lo[1], hi[1]);
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  lo = __builtin_amdgcn_permlane32_swap(static_cast<uint32_t>(w), static_cast<uint32_t>(w), false, false);
+  hi = __builtin_amdgcn_permlane32_swap(static_cast<uint32_t>(w >> 32), static_cast<uint32_t>(w >> 32), false, false);
+  return pair(lo[0], hi[0]) + pair(lo[1], hi[1]);
+}
+// Sum of v over this lane and those before it.
+__device__ __forceinline__ double wave_scan(double v) {
+  v += dpp<0x111>(v);       // row_shr:1, 2, 4, 8
+  v += dpp<0x112>(v);
+  v += dpp<0x114>(v);
+  v += dpp<0x118>(v);
+  v += dpp<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
+  v += dpp<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
+  return v;
+}
 
 struct Request {
   bool valid;    // its rows lie inside the logits
   int n_drafts;
   bool greedy;
-  double inv_t;
+  double c;      // log2(e) / T
   int64_t target_row, draft_row;
 };
 
@@ -105,7 +158,7 @@ __device__ __forceinline__ Request request_of(const span_verify_call& c, int q) 
   r.n_drafts = c.n_drafts ? max(0, min(c.n_drafts[q], k)) : k;
   const float t = c.temperature ? c.temperature[q] : 1.f;
   r.greedy = !(t > 0.f);
-  r.inv_t = r.greedy ? 1.0 : 1.0 / static_cast<double>(t);
+  r.c = r.greedy ? kLog2e : kLog2e / static_cast<double>(t);
   r.target_row = c.target_row0 ? c.target_row0[q] : static_cast<int64_t>(q) * (k + 1);
   r.draft_row = c.draft_row0 ? c.draft_row0[q] : static_cast<int64_t>(q) * k;
   r.valid = r.target_row >= 0 && r.target_row + r.n_drafts < c.target_rows &&
@@ -113,138 +166,142 @@ __device__ __forceinline__ Request request_of(const span_verify_call& c, int q) 
   return r;
 }
 
+// A lane's kPer logits of a chunk, four at a time (a vector of 16 bytes from any multiple of
+// four: rows of an odd vocabulary start anywhere); -inf past the vocabulary.
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ int id_of(int base, int lane, int u) { return base + 4 * (64 * (u / 4) + lane) + u % 4; }
+
+__device__ __forceinline__ void load_chunk(const float* __restrict__ row, int base, int lane, int vocab,
+                                           float (&x)[kPer]) {
+  if (base + kChunk <= vocab) {
+#pragma unroll
+    for (int u = 0; u < kPer; u += 4) {
+      const f32x4_any v = *reinterpret_cast<const f32x4_any*>(row + id_of(base, lane, u));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[u + e] = v[e];
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int i = id_of(base, lane, u);
+      x[u] = i < vocab ? row[i] : -INFINITY;
+    }
+  }
+}
+
 // ------------------------------------------------------------------ 1: chunks of every row
-template <bool kVec>
 __global__ __launch_bounds__(kThreads) void verify_stats_kernel(const Args a) {
-  __shared__ float s_max[kThreads / 64];
-  __shared__ int s_arg[kThreads / 64];
-  __shared__ double s_sum[kThreads / 64];
   const span_verify_call& c = a.c;
   const int q = a.q0 + static_cast<int>(blockIdx.z);
   const int k = c.max_drafts;
   const bool draft = static_cast<int>(blockIdx.y) > k;
   const int j = draft ? static_cast<int>(blockIdx.y) - k - 1 : static_cast<int>(blockIdx.y);
+  const int lane = threadIdx.x & 63;
+  const int chunk = blockIdx.x * kWaves + (threadIdx.x >> 6);
   const Request r = request_of(c, q);
-  if (!r.valid || (draft ? j >= r.n_drafts || r.greedy : j > r.n_drafts)) return;
+  if (chunk >= a.chunks || !r.valid || (draft ? j >= r.n_drafts || r.greedy : j > r.n_drafts)) return;
   const float* row = draft ? c.draft_logits + (r.draft_row + j) * c.draft_stride
                            : c.target_logits + (r.target_row + j) * c.target_stride;
-  const int base = blockIdx.x * kChunk;
+  const int base = chunk * kChunk;
   float x[kPer];
-  if constexpr (kVec) {
+  load_chunk(row, base, lane, c.vocab, x);
+  float best = x[0];
 #pragma unroll
-    for (int u = 0; u < kPer / 4; ++u) {
-      const int i = base + 4 * (u * kThreads + static_cast<int>(threadIdx.x));
-      if (i + 3 < c.vocab) {
-        const float4 v = *reinterpret_cast<const float4*>(row + i);
-        x[4 * u] = v.x;
-        x[4 * u + 1] = v.y;
-        x[4 * u + 2] = v.z;
-        x[4 * u + 3] = v.w;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * u + e] = i + e < c.vocab ? row[i + e] : -INFINITY;
-      }
-    }
-  } else {
-#pragma unroll
-    for (int u = 0; u < kPer; ++u) {
-      const int i = base + u * kThreads + static_cast<int>(threadIdx.x);
-      x[u] = i < c.vocab ? row[i] : -INFINITY;
-    }
-  }
-  float best = -INFINITY;
+  for (int u = 1; u < kPer; ++u) best = fmaxf(best, x[u]);
+  best = wave_max(best);
+  if (!(best > -INFINITY)) best = -INFINITY;  // a chunk of NaN
   int arg = INT32_MAX;
+  if (r.greedy) {
 #pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    const int i = kVec ? base + 4 * ((u / 4) * kThreads + static_cast<int>(threadIdx.x)) + u % 4
-                       : base + u * kThreads + static_cast<int>(threadIdx.x);
-    if (x[u] > best) {  // ids rise: an equal later one keeps the lower id
-      best = x[u];
-      arg = i;
-    }
+    for (int u = kPer - 1; u >= 0; --u)
+      if (x[u] == best) arg = id_of(base, lane, u);  // a lane's ids rise with u
+    arg = wave_min(arg);
   }
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) better(best, arg, __shfl_xor(best, off), __shfl_xor(arg, off));
-  const int wave = threadIdx.x >> 6;
-  if ((threadIdx.x & 63) == 0) {
-    s_max[wave] = best;
-    s_arg[wave] = arg;
-  }
-  __syncthreads();
-  best = s_max[0];
-  arg = s_arg[0];
-#pragma unroll
-  for (int w = 1; w < kThreads / 64; ++w) better(best, arg, s_max[w], s_arg[w]);
   double sum = 0.0;
+  if (best == INFINITY) {  // all the weight on the infinite ones
 #pragma unroll
-  for (int u = 0; u < kPer; ++u) sum += weight(x[u], best, r.inv_t);
+    for (int u = 0; u < kPer; ++u) sum += x[u] == best ? 1.0 : 0.0;
+  } else if (best > -INFINITY) {
+    const double max = best;
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) sum += shfl_xor_f64(sum, off);
-  if ((threadIdx.x & 63) == 0) s_sum[wave] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-#pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) sum += s_sum[w];
+    for (int u = 0; u < kPer; ++u) sum += exp2_neg((static_cast<double>(x[u]) - max) * r.c);
+  }
+  sum = wave_sum(sum);
+  if (lane == 0) {
     Stat* to = draft ? a.draft + (static_cast<int64_t>(q) * k + j) * a.chunks
                      : a.target + (static_cast<int64_t>(q) * (k + 1) + j) * a.chunks;
-    to[blockIdx.x] = Stat{sum, best, arg};
+    to[chunk] = Stat{sum, best, arg};
   }
 }
 
-// A row's largest logit, its lowest id and its sum of weights, by one wave.
-__device__ __forceinline__ Stat whole_row(const Stat* st, int chunks, double inv_t, int lane) {
-  float best = -INFINITY;
+// A row's largest logit, its lowest id (greedy requests) and its sum of weights, by one wave.
+__device__ __forceinline__ Stat whole_row(const Stat* st, int chunks, const Request& r, int lane) {
+  Stat mine{0.0, -INFINITY, INT32_MAX};
+  if (lane < chunks) mine = st[lane];
+  float best = mine.max;
+  for (int i = lane + 64; i < chunks; i += 64) best = fmaxf(best, st[i].max);
+  best = wave_max(best);
   int arg = INT32_MAX;
-  for (int i = lane; i < chunks; i += 64) better(best, arg, st[i].max, st[i].arg);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) better(best, arg, __shfl_xor(best, off), __shfl_xor(arg, off));
-  double sum = 0.0;
-  for (int i = lane; i < chunks; i += 64) sum += st[i].sum * weight(st[i].max, best, inv_t);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) sum += shfl_xor_f64(sum, off);
-  return Stat{sum, best, arg};
+  if (r.greedy) {
+    arg = mine.max == best ? mine.arg : INT32_MAX;
+    for (int i = lane + 64; i < chunks; i += 64)
+      if (st[i].max == best) arg = min(arg, st[i].arg);
+    arg = wave_min(arg);
+  }
+  double sum = mine.sum * weight(mine.max, best, r.c);
+  for (int i = lane + 64; i < chunks; i += 64) sum += st[i].sum * weight(st[i].max, best, r.c);
+  return Stat{wave_sum(sum), best, arg};
 }
 
 // What the work-groups of 2 and 3 need of a request's rows.
 struct Verdict {
   Stat p[kMaxDrafts + 1], q[kMaxDrafts];
+  float x[kMaxDrafts];  // the drafted tokens' logits
   int keep[kMaxDrafts];
 };
 
 // Acceptance of a request's drafts, by all waves of the work-group; returns the number
 // kept.  p and q of `v` hold the rows' sums afterwards.
-__device__ int accept(const Args& a, int q, const Request& r, Verdict& v, int waves) {
+template <int kNW>
+__device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Verdict& v) {
   const span_verify_call& c = a.c;
   const int k = c.max_drafts;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const bool dist = c.draft_logits && !r.greedy;
-  for (int e = wave; e < r.n_drafts + 1 + (dist ? r.n_drafts : 0); e += waves) {
-    if (e <= r.n_drafts) {
-      const Stat s = whole_row(a.target + (static_cast<int64_t>(q) * (k + 1) + e) * a.chunks, a.chunks, r.inv_t, lane);
-      if (lane == 0) v.p[e] = s;
-    } else {
-      const int j = e - r.n_drafts - 1;
-      const Stat s = whole_row(a.draft + (static_cast<int64_t>(q) * k + j) * a.chunks, a.chunks, r.inv_t, lane);
-      if (lane == 0) v.q[j] = s;
+  // the drafted tokens and their logits: asked for first, used last
+  const int mine = static_cast<int>(threadIdx.x);
+  int d = -1;
+  float x = 0.f, y = 0.f, u = 0.f;
+  if (mine < r.n_drafts) {
+    d = c.drafts[static_cast<int64_t>(q) * k + mine];
+    u = c.u_accept[static_cast<int64_t>(q) * k + mine];
+    if (d >= 0 && d < c.vocab) {
+      x = c.target_logits[(r.target_row + mine) * c.target_stride + d];
+      if (dist) y = c.draft_logits[(r.draft_row + mine) * c.draft_stride + d];
     }
   }
+  for (int e = wave; e < r.n_drafts + 1 + (dist ? r.n_drafts : 0); e += kNW) {
+    const bool of_p = e <= r.n_drafts;
+    const int j = of_p ? e : e - r.n_drafts - 1;
+    const Stat* st = of_p ? a.target + (static_cast<int64_t>(q) * (k + 1) + j) * a.chunks
+                          : a.draft + (static_cast<int64_t>(q) * k + j) * a.chunks;
+    const Stat s = whole_row(st, a.chunks, r, lane);
+    if (lane == 0) (of_p ? v.p[j] : v.q[j]) = s;
+  }
   __syncthreads();
-  for (int j = threadIdx.x; j < r.n_drafts; j += blockDim.x) {
-    const int d = c.drafts[static_cast<int64_t>(q) * k + j];
+  if (mine < r.n_drafts) {
+    const int j = mine;
     bool keep = false;
     if (r.greedy) {
       keep = v.p[j].sum > 0.0 && d == v.p[j].arg;
     } else if (d >= 0 && d < c.vocab) {
-      const float x = c.target_logits[(r.target_row + j) * c.target_stride + d];
-      const double pd = v.p[j].sum > 0.0 ? weight(x, v.p[j].max, r.inv_t) / v.p[j].sum : 0.0;
+      const double pd = v.p[j].sum > 0.0 ? weight(x, v.p[j].max, r.c) / v.p[j].sum : 0.0;
       double qd = 1.0;
-      if (dist) {
-        const float y = c.draft_logits[(r.draft_row + j) * c.draft_stride + d];
-        qd = v.q[j].sum > 0.0 ? weight(y, v.q[j].max, r.inv_t) / v.q[j].sum : 0.0;
-      }
-      keep = static_cast<double>(c.u_accept[static_cast<int64_t>(q) * k + j]) * qd < pd;
+      if (dist) qd = v.q[j].sum > 0.0 ? weight(y, v.q[j].max, r.c) / v.q[j].sum : 0.0;
+      keep = static_cast<double>(u) * qd < pd;
     }
     v.keep[j] = keep;
+    v.x[j] = x;
   }
   __syncthreads();
   int n = 0;
@@ -252,29 +309,30 @@ __device__ int accept(const Args& a, int q, const Request& r, Verdict& v, int wa
   return n;
 }
 
-// What the row that decides a request leaves of token i: max(p - q, 0), or p.
+__device__ __forceinline__ double inverse(double s) { return s > 0.0 ? 1.0 / s : 0.0; }
+
+// What the row that decides a request leaves of a token: max(p - q, 0), or p.
 struct Left {
   const float* x;
   const float* y;  // the draft's logits, or null
   float pm, qm;
-  double ps, qs, inv_t;  // 1 / sums
-  int one_hot;           // the token taken out of p where the draft has no distribution, -1: none
-  __device__ __forceinline__ double operator()(int i) const {
-    double w = weight(x[i], pm, inv_t) * ps;
-    if (y) w = fmax(w - weight(y[i], qm, inv_t) * qs, 0.0);
+  double ps, qs, c;  // 1 / sums
+  int one_hot;       // the token taken out of p where the draft has no distribution, -1: none
+  __device__ __forceinline__ double of(int i, float xi, float yi) const {
+    double w = weight(xi, pm, c) * ps;
+    if (y) w = fmax(w - weight(yi, qm, c) * qs, 0.0);
     return i == one_hot ? 0.0 : w;
   }
 };
 
-__device__ __forceinline__ double inverse(double s) { return s > 0.0 ? 1.0 / s : 0.0; }
-
+// At the first refused draft n, or (plain, or after the last draft) p_n itself.
 __device__ __forceinline__ Left left_of(const Args& a, int q, const Request& r, const Verdict& v, int n, bool plain) {
   const span_verify_call& c = a.c;
   Left l{};
   l.x = c.target_logits + (r.target_row + n) * c.target_stride;
   l.pm = v.p[n].max;
   l.ps = inverse(v.p[n].sum);
-  l.inv_t = r.inv_t;
+  l.c = r.c;
   l.one_hot = -1;
   if (n < r.n_drafts && !plain) {
     if (c.draft_logits) {
@@ -292,174 +350,132 @@ __device__ __forceinline__ Left left_of(const Args& a, int q, const Request& r, 
 // ------------------------------------------------------------------ 2: what the deciding row leaves
 __global__ __launch_bounds__(kThreads) void verify_left_kernel(const Args a) {
   __shared__ Verdict v;
-  __shared__ double s_sum[kThreads / 64];
   const span_verify_call& c = a.c;
   const int q = a.q0 + static_cast<int>(blockIdx.y);
+  const int lane = threadIdx.x & 63;
   const Request r = request_of(c, q);
   if (!r.valid || r.greedy || r.n_drafts == 0) return;
-  const int n = accept(a, q, r, v, kThreads / 64);
-  if (n == r.n_drafts) return;  // after the last draft the chunks' own sums serve
+  const int n = accept<kWaves>(a, q, r, v);
+  const int chunk = blockIdx.x * (kWaves) + (threadIdx.x >> 6);
+  if (n == r.n_drafts || chunk >= a.chunks) return;  // after the last draft the chunks' own sums serve
   const Left l = left_of(a, q, r, v, n, false);
+  const int base = chunk * kChunk;
+  float x[kPer], y[kPer];
+  load_chunk(l.x, base, lane, c.vocab, x);
+  load_chunk(l.y, base, lane, c.vocab, y);
   double sum = 0.0;
-  for (int u = 0; u < kPer; ++u) {
-    const int i = blockIdx.x * kChunk + u * kThreads + static_cast<int>(threadIdx.x);
-    if (i < c.vocab) sum += l(i);
-  }
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) sum += shfl_xor_f64(sum, off);
-  if ((threadIdx.x & 63) == 0) s_sum[threadIdx.x >> 6] = sum;
-  __syncthreads();
-  if (threadIdx.x == 0) {
-#pragma unroll
-    for (int w = 1; w < kThreads / 64; ++w) sum += s_sum[w];
-    a.left[static_cast<int64_t>(q) * a.chunks + blockIdx.x] = sum;
-  }
-}
-
-// Sum of v over the threads before this one, and over all of them.
-__device__ __forceinline__ double scan_before(double v, double* total, double* s_wave) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  double inc = v;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const double o = __shfl_up(inc, off);
-    if (lane >= off) inc += o;
-  }
-  if (lane == 63) s_wave[wave] = inc;
-  __syncthreads();
-  double before = 0.0, all = 0.0;
-  for (int w = 0; w < kPickThreads / 64; ++w) {
-    if (w == wave) before = all;
-    all += s_wave[w];
-  }
-  __syncthreads();
-  *total = all;
-  const double up = __shfl_up(inc, 1);
-  return before + (lane > 0 ? up : 0.0);
+  for (int u = 0; u < kPer; ++u) sum += l.of(-2, x[u], y[u]);
+  sum = wave_sum(sum);
+  if (lane == 0) a.left[static_cast<int64_t>(q) * a.chunks + chunk] = sum;
 }
 
 // ------------------------------------------------------------------ 3: the token
 __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a) {
+  constexpr int kPickWaves = kPickThreads / 64;
+  constexpr int kEach = kChunk / kPickThreads;
   __shared__ Verdict v;
-  __shared__ double s_wave[kPickThreads / 64];
+  __shared__ double s_wave[kPickWaves];
   __shared__ int s_first, s_last;
-  __shared__ double s_before;
   const span_verify_call& c = a.c;
   const int q = a.q0 + static_cast<int>(blockIdx.x);
   const int k = c.max_drafts;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Request r = request_of(c, q);
   int32_t* tokens = c.tokens + static_cast<int64_t>(q) * (k + 1);
   float* lps = c.logprobs ? c.logprobs + static_cast<int64_t>(q) * (k + 1) : nullptr;
   if (!r.valid) {
-    for (int j = threadIdx.x; j <= k; j += kPickThreads) {
-      tokens[j] = -1;
-      if (lps) lps[j] = 0.f;
+    if (static_cast<int>(threadIdx.x) <= k) {
+      tokens[threadIdx.x] = -1;
+      if (lps) lps[threadIdx.x] = 0.f;
     }
     if (threadIdx.x == 0) c.accepted[q] = -1;
     return;
   }
-  const int n = accept(a, q, r, v, kPickThreads / 64);
-  int token = -1;
-  if (r.greedy) {
-    token = v.p[n].sum > 0.0 ? v.p[n].arg : -1;
-  } else if (v.p[n].sum > 0.0) {
-    const double u = static_cast<double>(c.u_sample[q]);
-    const Stat* st = a.target + (static_cast<int64_t>(q) * (k + 1) + n) * a.chunks;
-    bool plain = n == r.n_drafts;
-    // chunk sums in order: the first chunk whose running sum passes u times the whole
-    for (;;) {
-      const Left l = left_of(a, q, r, v, n, plain);
-      const double* left = !plain && l.y ? a.left + static_cast<int64_t>(q) * a.chunks : nullptr;
-      double total = 0.0, run = 0.0;
-      auto chunk_sum = [&](int i) -> double {
-        if (left) return left[i];
-        double s = st[i].sum * weight(st[i].max, l.pm, r.inv_t) * l.ps;
-        if (l.one_hot >= 0 && l.one_hot / kChunk == i) {
-          s -= weight(l.x[l.one_hot], l.pm, r.inv_t) * l.ps;
-          s = s > 0.0 ? s : 0.0;
-        }
-        return s;
-      };
-      // the whole, then the chunk: kPickThreads chunks at a time
-      for (int b = 0; b < a.chunks; b += kPickThreads) {
-        const int i = b + static_cast<int>(threadIdx.x);
-        double all;
-        (void)scan_before(i < a.chunks ? chunk_sum(i) : 0.0, &all, s_wave);
-        total += all;
-      }
-      if (!(total > 0.0) && !plain) {  // nothing left of p: p itself
-        plain = true;
-        continue;
-      }
-      const double target = u * total;
-      if (threadIdx.x == 0) {
-        s_first = INT32_MAX;
-        s_last = -1;
-      }
-      __syncthreads();
-      for (int b = 0; b < a.chunks; b += kPickThreads) {
-        const int i = b + static_cast<int>(threadIdx.x);
-        const double w = i < a.chunks ? chunk_sum(i) : 0.0;
-        double all;
-        const double before = run + scan_before(w, &all, s_wave);
-        if (w > 0.0) {
-          if (before + w > target) atomicMin(&s_first, i);
-          atomicMax(&s_last, i);
-        }
-        run += all;
-      }
-      __syncthreads();
-      const int chunk = s_first != INT32_MAX ? s_first : s_last;
-      __syncthreads();
-      run = 0.0;
-      for (int b = 0; b < a.chunks; b += kPickThreads) {
-        const int i = b + static_cast<int>(threadIdx.x);
-        double all;
-        const double before = run + scan_before(i < a.chunks ? chunk_sum(i) : 0.0, &all, s_wave);
-        if (i == chunk) s_before = before;
-        run += all;
-      }
-      if (threadIdx.x == 0) {
-        s_first = INT32_MAX;
-        s_last = -1;
-      }
-      __syncthreads();
-      // the token in the chunk: each thread four tokens that follow one another
-      constexpr int kEach = kChunk / kPickThreads;
-      const int i0 = chunk * kChunk + static_cast<int>(threadIdx.x) * kEach;
-      double w[kEach], mine = 0.0;
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        w[e] = i0 + e < c.vocab ? l(i0 + e) : 0.0;
-        mine += w[e];
-      }
-      double all;
-      double at = s_before + scan_before(mine, &all, s_wave);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        at += w[e];
-        if (w[e] > 0.0) {
-          if (at > target) atomicMin(&s_first, i0 + e);
-          atomicMax(&s_last, i0 + e);
-        }
-      }
-      __syncthreads();
-      token = s_first != INT32_MAX ? s_first : s_last;
-      break;
-    }
+  if (threadIdx.x == 0) {
+    s_first = INT32_MAX;
+    s_last = -1;
   }
-  for (int j = threadIdx.x; j <= k; j += kPickThreads) {
-    int t = -1;
-    if (j < n) t = c.drafts[static_cast<int64_t>(q) * k + j];
-    if (j == n) t = token;
+  const float u_sample = c.u_sample[q];
+  const int n = accept<kPickWaves>(a, q, r, v);  // (its barriers also publish s_first and s_last)
+  int token = -1;
+  if (!(v.p[n].sum > 0.0)) {
+  } else if (r.greedy) {
+    token = v.p[n].arg;
+  } else {
+    const Stat* st = a.target + (static_cast<int64_t>(q) * (k + 1) + n) * a.chunks;
+    // Every wave finds the chunk for itself: the first one whose running sum passes u times
+    // the whole, else the last with any weight.
+    Left l = left_of(a, q, r, v, n, false);
+    double aim = 0.0, before = 0.0;
+    int chunk = -1;
+    for (int attempt = 0; attempt < 2 && chunk < 0; ++attempt) {
+      if (attempt == 1) l = left_of(a, q, r, v, n, true);  // nothing left of p: p itself
+      auto chunk_sum = [&](int i) -> double {
+        if (i >= a.chunks) return 0.0;
+        if (l.y) return a.left[static_cast<int64_t>(q) * a.chunks + i];
+        double s = st[i].sum * weight(st[i].max, l.pm, l.c) * l.ps;
+        if (l.one_hot >= 0 && l.one_hot / kChunk == i) s -= weight(l.x[l.one_hot], l.pm, l.c) * l.ps;
+        return s > 0.0 ? s : 0.0;
+      };
+      const double own = chunk_sum(lane);  // all of them up to 64 chunks
+      double total = 0.0;
+      for (int b = 0; b < a.chunks; b += 64) total += wave_sum(b == 0 ? own : chunk_sum(b + lane));
+      aim = static_cast<double>(u_sample) * total;
+      double run = 0.0;
+      for (int b = 0; b < a.chunks; b += 64) {
+        const double w = b == 0 ? own : chunk_sum(b + lane);
+        const double upto = run + wave_scan(w);
+        const unsigned long long some = __ballot(w > 0.0), past = __ballot(w > 0.0 && upto > aim);
+        // the first that passes; while none does, the last with weight
+        const int at = past ? __ffsll(past) - 1 : some ? 63 - __clzll(some) : -1;
+        if (at >= 0) {
+          chunk = b + at;
+          before = __shfl(upto, at) - __shfl(w, at);
+        }
+        if (past) break;
+        run = __shfl(upto, 63);
+      }
+    }
+    // the token in the chunk: each thread tokens that follow one another
+    const int i0 = chunk * kChunk + static_cast<int>(threadIdx.x) * kEach;
+    double w[kEach], mine = 0.0;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      const bool in = i0 + e < c.vocab;
+      w[e] = in ? l.of(i0 + e, l.x[i0 + e], l.y ? l.y[i0 + e] : 0.f) : 0.0;
+      mine += w[e];
+    }
+    const double upto = wave_scan(mine);
+    if (lane == 63) s_wave[wave] = upto;
+    __syncthreads();
+    double at = before + upto - mine;
+    for (int e = 0; e < wave; ++e) at += s_wave[e];
+    int first = INT32_MAX, last = -1;
+#pragma unroll
+    for (int e = kEach - 1; e >= 0; --e)
+      if (w[e] > 0.0) last = max(last, i0 + e);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      at += w[e];
+      if (w[e] > 0.0 && at > aim) first = min(first, i0 + e);
+    }
+    if (first != INT32_MAX) atomicMin(&s_first, first);
+    if (last >= 0) atomicMax(&s_last, last);
+    __syncthreads();
+    token = s_first != INT32_MAX ? s_first : s_last;
+  }
+  const int j = static_cast<int>(threadIdx.x);
+  if (j <= k) {
+    const int t = j < n ? c.drafts[static_cast<int64_t>(q) * k + j] : j == n ? token : -1;
     tokens[j] = t;
     if (lps) {
       float lp = 0.f;
       if (t >= 0) {
-        const float x = c.target_logits[(r.target_row + j) * c.target_stride + t];
-        // a weight that is 1 (the largest logit) has no difference to scale
-        const double d = x == v.p[j].max ? 0.0 : (static_cast<double>(x) - static_cast<double>(v.p[j].max)) * r.inv_t;
-        lp = static_cast<float>(d - log(v.p[j].sum));
+        const float x = j < n ? v.x[j] : c.target_logits[(r.target_row + j) * c.target_stride + t];
+        // the largest logit (an infinite one too) has no difference to scale
+        const double d = x == v.p[j].max ? 0.0 : (static_cast<double>(x) - static_cast<double>(v.p[j].max)) * r.c;
+        lp = static_cast<float>(d * 0.69314718055994530942 - log(v.p[j].sum));
       }
       lps[j] = lp;
     }
@@ -484,22 +500,17 @@ hipError_t launch_verify_drafts(const span_verify_call& c, hipStream_t s) {
   a.target = static_cast<Stat*>(c.workspace);
   a.draft = a.target + n * (k + 1) * ch;
   a.left = reinterpret_cast<double*>(a.draft + n * k * ch);
-  const bool vec = reinterpret_cast<uintptr_t>(c.target_logits) % 16 == 0 && c.target_stride % 4 == 0 &&
-                   (!c.draft_logits || (reinterpret_cast<uintptr_t>(c.draft_logits) % 16 == 0 && c.draft_stride % 4 == 0));
   const unsigned rows = static_cast<unsigned>(c.max_drafts + 1 + (c.draft_logits ? c.max_drafts : 0));
   // requests on the grid's last dimension: as many at once as it takes
-  const int64_t threads = std::max<int64_t>(static_cast<int64_t>(a.chunks) * rows * kThreads, int64_t{1} << 17);
+  const int64_t threads = std::max<int64_t>((a.chunks + kWaves - 1) / kWaves * static_cast<int64_t>(rows) * kThreads, int64_t{1} << 17);
   return launch_in_slices(c.n_requests, threads, hipErrorInvalidValue, [&](int64_t first, int64_t count) -> hipError_t {
     a.q0 = static_cast<int>(first);
     const unsigned nq = static_cast<unsigned>(count);
-    if (vec) {
-      verify_stats_kernel<true><<<dim3(a.chunks, rows, nq), kThreads, 0, s>>>(a);
-    } else {
-      verify_stats_kernel<false><<<dim3(a.chunks, rows, nq), kThreads, 0, s>>>(a);
-    }
+    const unsigned groups = static_cast<unsigned>((a.chunks + kWaves - 1) / kWaves);
+    verify_stats_kernel<<<dim3(groups, rows, nq), kThreads, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && c.draft_logits && c.max_drafts > 0) {
-      verify_left_kernel<<<dim3(a.chunks, nq), kThreads, 0, s>>>(a);
+      verify_left_kernel<<<dim3(groups, nq), kThreads, 0, s>>>(a);
       e = hipGetLastError();
     }
     if (e != hipSuccess) return e;

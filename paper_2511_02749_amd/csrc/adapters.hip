@@ -2,28 +2,29 @@
 //
 //   out[i] = base[i] + scale[a] (x[i] A[a]^T) B[a]^T,   a = ids[i], rows without one copied
 //
-// in two launches.  Shrink: H = x A^T, sums of K products in fp32 split over the work-group's
-// waves (and over work-groups when there are few row tiles), partials in the workspace.
-// Expand: the partials summed in slice order, the product with B, scale and base added,
-// rounded once.
+// Shrink: H = x A^T, sums of K products in fp32 split over a work-group's waves and over
+// work-groups, each slice's partial in the workspace.  Expand: the partials summed in slice
+// order, the product with B, scale and base added, rounded once.  Between them, for many
+// rows, the partials are summed once (finish), where few rows' expand does it as it goes.
 //
-// Rows come in tiles of 16 in the caller's order, whatever their adapters: a tile is worked
-// once for each adapter that occurs in it (the group of its first row, the leader), and
-// only that group's rows are written.  So nothing is sorted, ids stay on the device and may
-// change between replays of a captured call.  The few-row form puts the groups of a tile on the grid
-// (a decode step has up to 16 adapters in a tile, all independent), the many-row form walks
-// them (a prefilled tile mostly has one).
+// Few rows (a decode step, kFewRows at most): the rows of one adapter, up to 16 at a time,
+// wherever they lie in the call, are one group, found from the ids by the work-groups
+// themselves, so that each adapter's weights are read once.  Many rows (prefilled
+// segments): tiles of 64 in the caller's order, worked once for each adapter that occurs in
+// one, mostly one.  So nothing is sorted, ids stay on the device and may change between
+// replays of a captured call.
 //
-// Matrix instructions 16x16x32: the weights are the A operand, the rows the B operand, so
-// that a lane ends with four consecutive columns of one row.  H goes into the second product
-// as two bf16 numbers, high and low part (16 significant bits), side by side in the 32 deep
-// reduction over the same 16 weights, which costs nothing: the instruction is 32 deep and a
-// block of ranks 16.
+// Matrix instructions 16x16x32, every operand 16 bytes of a row.  The second product's
+// columns are dealt to its tiles so that a lane's results of all tiles are columns that
+// follow one another, and base and out go as whole lines.  H enters it as two bf16 numbers, high and
+// low part (16 significant bits), side by side in the 32 deep reduction over the same 16
+// ranks, which costs nothing: the instruction is 32 deep and a block of ranks 16.
 //
 // Bound: HBM (x, base and out for many rows, A and B for few); 2 R (K P + N) operations a row.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "dev_common.h"
 #include "mfma_common.h"
@@ -36,10 +37,20 @@ using mfma::hi_bf16;
 using mfma::lo_bf16;
 using mfma::pack_bf16x2;
 
-constexpr int kTile = 16;     // rows of a tile
-constexpr int kShrinkWaves = 8;
-constexpr int kGroupCols = 4;  // 16-column tiles of H that one shrink work-group forms
-constexpr int kFewRows = 256;  // up to here the groups of a tile are on the grid
+constexpr int kTile = 16;      // rows of a group, ranks of a block
+constexpr int kFewRows = 256;  // up to here the rows are grouped by adapter
+constexpr int kFewSlices = 8;  // work-groups over K for few rows, whose partials expand adds up
+constexpr int kManySlices = 16;
+constexpr int kManyTiles = 4;  // 16-row tiles of a many-row work-group
+
+// Shrink work-groups: waves (each with its own part of K), 16-row and 16-column tiles of H,
+// and products of 32 values whose loads are in flight together.
+struct FewShrink {
+  static constexpr int kWaves = 8, kRows = 1, kCols = 1, kSteps = 4;
+};
+struct ManyShrink {
+  static constexpr int kWaves = 4, kRows = kManyTiles, kCols = 4, kSteps = 2;
+};
 
 struct Shape {
   const bf16_t* x;
@@ -50,115 +61,208 @@ struct Shape {
   const bf16_t* b;
   const float* scale;
   const int32_t* ranks;
-  float* h;  // [slices][rows][h_cols]
+  float* part;   // [slices][rows][h_cols] fp32
+  bf16_t* h;     // many rows: [rows][h_cols / 16][high 16, low 16]
   int64_t rows, x_stride, base_stride, out_stride;
   int K, R, n_adapters, n_parts;
   int N;         // columns of all parts
   int cols[4];   // columns of each part
   int rank_blocks, h_cols;  // ceil(R / 16); 16 * n_parts * rank_blocks
   int slices, k_slice;
+  int run;  // tiles of 16 rows that an expand work-group of many rows takes
 };
 
-// The adapter of tile row `lane & 15`, -1 for none.
-__device__ __forceinline__ int tile_id(const Shape& s, int64_t row0, int lane) {
-  const int64_t row = row0 + (lane & 15);
+__device__ __forceinline__ int adapter_of(const Shape& s, int64_t row) {
   const int id = row < s.rows ? s.ids[row] : -1;
   return id >= 0 && id < s.n_adapters ? id : -1;
 }
+
+// (a scalar, so that what follows from it is one too)
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
 
 __device__ __forceinline__ int rank_of(const Shape& s, int id) {
   return s.ranks ? max(0, min(s.ranks[id], s.R)) : s.R;
 }
 
-// Groups of a tile: f(adapter, rows of the group as a mask) for the group that row j leads
-// (j >= 0) or for every group (j < 0).  Wave-uniform.
+// The group that row j of few rows leads: rows of its adapter from j on, the first 16, if
+// as many of them as make whole groups lie before j.  Fills rows[0 .. n) and returns n, 0 if
+// j leads none.  Called by all threads; every wave finds it, wave 0 writes it.
+__device__ __forceinline__ int few_group(const Shape& s, int j, int* aid, int* rows) {
+  const int lane = threadIdx.x & 63;
+  const int mine = adapter_of(s, j);
+  *aid = mine;
+  const int n_rows = static_cast<int>(s.rows);
+  int id[kFewRows / 64];
+#pragma unroll
+  for (int b = 0; b < kFewRows / 64; ++b) id[b] = 64 * b < n_rows ? adapter_of(s, 64 * b + lane) : -1;
+  int before = 0, n = 0;
+#pragma unroll
+  for (int b = 0; b < kFewRows / 64; ++b) {
+    const int row = 64 * b + lane;
+    const bool same = row < n_rows && id[b] == mine;
+    before += __popcll(__ballot(same && row < j));
+    const unsigned long long later = __ballot(same && row >= j);
+    const int at = n + __popcll(later & ((1ull << lane) - 1));
+    if (threadIdx.x < 64 && same && row >= j && at < kTile) rows[at] = row;
+    n += __popcll(later);
+  }
+  __syncthreads();
+  return before % kTile == 0 ? min(n, kTile) : 0;
+}
+
+// The adapters of 64 rows (lane i: row i), each with its rows as a mask: f(adapter, rows).
+// Wave-uniform.
 template <class F>
-__device__ __forceinline__ void for_groups(int id, unsigned live, int j, F f) {
-  unsigned left = live;
-  while (left) {
-    const int first = j < 0 ? __ffs(left) - 1 : j;
-    if (!((live >> first) & 1)) return;
-    const int aid = __builtin_amdgcn_readlane(id, first);
-    const unsigned mine = static_cast<unsigned>(__ballot(id == aid)) & live;
-    if (j >= 0 && (mine & ((1u << j) - 1))) return;  // another row leads
+__device__ __forceinline__ void for_adapters(int id, unsigned long long live, F f) {
+  while (live) {
+    const int aid = __builtin_amdgcn_readlane(id, __ffsll(live) - 1);
+    const unsigned long long mine = __ballot(id == aid) & live;
     f(aid, mine);
-    if (j >= 0) return;
-    left &= ~mine;
+    live &= ~mine;
   }
 }
 
 __device__ __forceinline__ bf16x8_t as_frag(const uint4& v) { return __builtin_bit_cast(bf16x8_t, v); }
 
-// H partials of one tile, one slice of K and kGroupCols column tiles.
-__global__ __launch_bounds__(64 * kShrinkWaves) void adapter_shrink_kernel(const Shape s, bool few) {
-  __shared__ float4 red[kShrinkWaves][kGroupCols][kTile][4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int col_groups = (s.h_cols / 16 + kGroupCols - 1) / kGroupCols;
-  const int slice = blockIdx.x / col_groups, ct0 = (blockIdx.x % col_groups) * kGroupCols;
-  const int n_ct = min(kGroupCols, s.h_cols / 16 - ct0);
-  const int64_t row0 = static_cast<int64_t>(blockIdx.y) * kTile;
-  const int n_rows = static_cast<int>(min<int64_t>(kTile, s.rows - row0));
-  const int id = tile_id(s, row0, lane);
-  const int sub = s.k_slice / kShrinkWaves;  // a multiple of 64
+// A float as the nearest bf16 and what that leaves of it (none of a value that is not finite),
+// for two of them packed.
+__device__ __forceinline__ void split2(float a, float b, uint32_t* high, uint32_t* low) {
+  *high = pack_bf16x2(a, b);
+  const float l0 = a - lo_bf16(*high), l1 = b - hi_bf16(*high);
+  *low = pack_bf16x2(isfinite(l0) ? l0 : 0.f, isfinite(l1) ? l1 : 0.f);
+}
+
+// Four sums of H as their high and low parts, ranks 4 q .. of a block at h.
+__device__ __forceinline__ void store_split(bf16_t* h, int q, const float4& sum) {
+  uint2 high, low;
+  split2(sum.x, sum.y, &high.x, &low.x);
+  split2(sum.z, sum.w, &high.y, &low.y);
+  reinterpret_cast<uint2*>(h)[q] = high;
+  reinterpret_cast<uint2*>(h)[q + 4] = low;
+}
+
+__device__ __forceinline__ float4 operator+(const float4& a, const float4& b) {
+  return float4{a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w};
+}
+
+// H of one group (few) or of a tile of 64 rows: one slice of K, C::kCols column tiles.
+template <bool kFew, class C>
+__global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Shape s) {
+  __shared__ float4 red[C::kWaves][C::kCols][16 * C::kRows][4];
+  __shared__ int list[kTile];
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  const int col_groups = (s.h_cols / 16 + C::kCols - 1) / C::kCols;
+  const int slice = blockIdx.x / col_groups, ct0 = (blockIdx.x % col_groups) * C::kCols;
+  const int n_ct = min(C::kCols, s.h_cols / 16 - ct0);
+  const int sub = s.k_slice / C::kWaves;
   const int k0 = slice * s.k_slice + wave * sub;
   const int k1 = min(s.K, k0 + sub);
   const int m = lane & 15, g = lane >> 4;
-  for_groups(id, (1u << n_rows) - 1, few ? static_cast<int>(blockIdx.z) : -1, [&](int aid, unsigned mine) {
-    if (aid < 0) return;
+  // row_at(i): row of the call of row i of the group or tile
+  auto work = [&](int aid, unsigned long long mine, auto row_at) {
     const int rank = rank_of(s, aid);
-    const bool has_row = (mine >> m) & 1;
-    const bf16_t* xp = s.x + (row0 + m) * s.x_stride;
-    const bf16_t* ap[kGroupCols];
-    bool has_w[kGroupCols];
+    // Rows outside the group and ranks past the adapter's are read as the group's first row and
+    // rank: no result of theirs is used, and no load needs a branch.
+    const int row1 = __ffsll(mine) - 1;
+    const bf16_t* xp[C::kRows];
 #pragma unroll
-    for (int c = 0; c < kGroupCols; ++c) {
-      const int ct = ct0 + c, p = ct / s.rank_blocks, r = (ct - p * s.rank_blocks) * 16 + m;
-      has_w[c] = c < n_ct && r < rank;
-      ap[c] = s.a + ((static_cast<int64_t>(aid) * s.n_parts + p) * s.R + r) * s.K;
+    for (int t = 0; t < C::kRows; ++t)
+      xp[t] = s.x + row_at((mine >> (16 * t + m)) & 1 ? 16 * t + m : row1) * s.x_stride + 8 * g;
+    const bf16_t* ap[C::kCols];
+#pragma unroll
+    for (int c = 0; c < C::kCols; ++c) {
+      const int ct = ct0 + min(c, n_ct - 1), p = ct / s.rank_blocks, r = (ct - p * s.rank_blocks) * 16 + m;
+      ap[c] = s.a + ((static_cast<int64_t>(aid) * s.n_parts + p) * s.R + (r < rank ? r : 0)) * s.K + 8 * g;
     }
-    f32x4_t acc[kGroupCols] = {};
-    for (int k = k0; k < k1; k += 64) {
-      // lane group g covers k + 16 g .. + 15: the same order in both operands
-      uint4 xv[2], wv[kGroupCols][2];
+    f32x4_t acc[C::kRows][C::kCols] = {};
+    uint4 xv[C::kRows][C::kSteps], wv[C::kCols][C::kSteps];
+    auto multiply = [&] {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int kk = k + 16 * g + 8 * t;
-        xv[t] = uint4{0u, 0u, 0u, 0u};
-        if (has_row && kk < k1) xv[t] = *reinterpret_cast<const uint4*>(xp + kk);
+      for (int u = 0; u < C::kSteps; ++u)
 #pragma unroll
-        for (int c = 0; c < kGroupCols; ++c) {
-          wv[c][t] = uint4{0u, 0u, 0u, 0u};
-          if (has_w[c] && kk < k1) wv[c][t] = *reinterpret_cast<const uint4*>(ap[c] + kk);
+        for (int t = 0; t < C::kRows; ++t)
+#pragma unroll
+          for (int c = 0; c < C::kCols; ++c)
+            acc[t][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(wv[c][u]), as_frag(xv[t][u]), acc[t][c], 0, 0, 0);
+    };
+    int k = k0;
+    for (; k + 32 * C::kSteps <= k1; k += 32 * C::kSteps) {
+#pragma unroll
+      for (int u = 0; u < C::kSteps; ++u) {
+#pragma unroll
+        for (int t = 0; t < C::kRows; ++t) xv[t][u] = *reinterpret_cast<const uint4*>(xp[t] + k + 32 * u);
+#pragma unroll
+        for (int c = 0; c < C::kCols; ++c) wv[c][u] = *reinterpret_cast<const uint4*>(ap[c] + k + 32 * u);
+      }
+      multiply();
+    }
+    if (k < k1) {  // the end of a K that is no multiple
+#pragma unroll
+      for (int u = 0; u < C::kSteps; ++u) {
+        const bool in = k + 32 * u + 8 * g < k1;
+#pragma unroll
+        for (int t = 0; t < C::kRows; ++t) {
+          xv[t][u] = uint4{0u, 0u, 0u, 0u};
+          if (in) xv[t][u] = *reinterpret_cast<const uint4*>(xp[t] + k + 32 * u);
+        }
+#pragma unroll
+        for (int c = 0; c < C::kCols; ++c) {
+          wv[c][u] = uint4{0u, 0u, 0u, 0u};
+          if (in) wv[c][u] = *reinterpret_cast<const uint4*>(ap[c] + k + 32 * u);
         }
       }
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int c = 0; c < kGroupCols; ++c)
-          acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(wv[c][t]), as_frag(xv[t]), acc[c], 0, 0, 0);
+      multiply();
     }
+    // a lane holds ranks 4 g .. of row m of each tile
 #pragma unroll
-    for (int c = 0; c < kGroupCols; ++c)
-      if (c < n_ct) red[wave][c][m][g] = __builtin_bit_cast(float4, acc[c]);
+    for (int t = 0; t < C::kRows; ++t)
+#pragma unroll
+      for (int c = 0; c < C::kCols; ++c)
+        if (c < n_ct) red[wave][c][16 * t + m][g] = __builtin_bit_cast(float4, acc[t][c]);
     __syncthreads();
-    for (int e = threadIdx.x; e < n_ct * kTile * 4; e += 64 * kShrinkWaves) {
-      const int q = e & 3, row = (e >> 2) & 15, c = e >> 6;
-      if ((mine >> row) & 1) {
-        float4 sum = red[0][c][row][q];
+    for (int e = threadIdx.x; e < n_ct * 64 * C::kRows; e += 64 * C::kWaves) {
+      const int q = e & 3, row = (e >> 2) % (16 * C::kRows), c = e / (64 * C::kRows);
+      if (!((mine >> row) & 1)) continue;
+      float4 sum = red[0][c][row][q];
 #pragma unroll
-        for (int w = 1; w < kShrinkWaves; ++w) {
-          const float4 v = red[w][c][row][q];
-          sum.x += v.x;
-          sum.y += v.y;
-          sum.z += v.z;
-          sum.w += v.w;
-        }
-        *reinterpret_cast<float4*>(s.h + (static_cast<int64_t>(slice) * s.rows + row0 + row) * s.h_cols +
-                                   (ct0 + c) * 16 + 4 * q) = sum;
-      }
+      for (int w = 1; w < C::kWaves; ++w) sum = sum + red[w][c][row][q];
+      const int64_t to = row_at(row);
+      const int r = (ct0 + c) % s.rank_blocks * 16 + 4 * q;  // past the rank H is zero
+      sum = float4{r < rank ? sum.x : 0.f, r + 1 < rank ? sum.y : 0.f, r + 2 < rank ? sum.z : 0.f, r + 3 < rank ? sum.w : 0.f};
+      if (!kFew && s.slices == 1)
+        store_split(s.h + 2 * (to * s.h_cols + (ct0 + c) * 16), q, sum);
+      else
+        *reinterpret_cast<float4*>(s.part + (slice * s.rows + to) * s.h_cols + (ct0 + c) * 16 + 4 * q) = sum;
     }
     __syncthreads();
-  });
+  };
+  if constexpr (kFew) {
+    int aid = 0;
+    const int n = few_group(s, blockIdx.y, &aid, list);
+    if (n > 0 && aid >= 0) work(aid, (1ull << n) - 1, [&](int i) -> int64_t { return list[i]; });
+  } else {
+    const int64_t row0 = static_cast<int64_t>(blockIdx.y) * (16 * C::kRows);
+    const int64_t row = row0 + lane;
+    const unsigned long long live = __ballot(row < s.rows);
+    for_adapters(adapter_of(s, row), live, [&](int aid, unsigned long long mine) {
+      if (aid >= 0) work(aid, mine, [&](int i) -> int64_t { return row0 + i; });
+    });
+  }
+}
+
+// Many rows: the slices' partials of H added up, as high and low parts.
+__global__ __launch_bounds__(256) void adapter_finish_kernel(const Shape s) {
+  const int64_t plane = s.rows * s.h_cols / 4;  // in vectors of four
+  const int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+  if (e >= plane) return;
+  const float4* p = reinterpret_cast<const float4*>(s.part) + e;
+  float4 v[kManySlices];
+#pragma unroll
+  for (int i = 0; i < kManySlices; ++i) v[i] = i < s.slices ? p[i * plane] : float4{0.f, 0.f, 0.f, 0.f};
+  float4 sum = v[0];
+#pragma unroll
+  for (int i = 1; i < kManySlices; ++i) sum = sum + v[i];
+  store_split(s.h + 32 * (e / 4), static_cast<int>(e & 3), sum);
 }
 
 // Zeroes elements n .. 7 of eight bf16 values.
@@ -173,109 +277,271 @@ __device__ __forceinline__ uint4 first_of(const uint4& v, int n) {
 }
 
 constexpr int kExpandWaves = 4;
-constexpr int kWaveCols = 64;
 
-// Columns [256 b, 256 b + 256) of one part for one tile of rows (few) or `tiles` tiles.
-__global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_kernel(const Shape s, bool few, int tiles) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int m = lane & 15, g = lane >> 4;
-  int block = blockIdx.x, part = 0, col0 = 0;
-  for (; part < s.n_parts - 1; ++part) {
-    const int nb = (s.cols[part] + kExpandWaves * kWaveCols - 1) / (kExpandWaves * kWaveCols);
+// The wave's columns of one part, n0 .. of `width`, and where they lie in all columns.
+struct Cols {
+  int part, n0, width, col0;
+};
+
+// J tiles of 16 columns: column m of tile j is column J m + j of the wave's, so that a lane's
+// results are J columns that follow one another.
+template <int J>
+struct Out {
+  using Vec = std::conditional_t<J == 8, uint4, uint2>;
+  // Ranks r0 .. r0 + 7 of tile j's weights, those past `rank` zero.  Columns past the part's
+  // and ranks past R are read as its first ones: no result of theirs is used.
+  static __device__ __forceinline__ uint4 weights(const Shape& s, const Cols& c, int aid, int j, int m, int r0,
+                                                  int rank, bool whole) {
+    const int col = c.n0 + J * m < c.width ? c.n0 + J * m + j : j;
+    // (columns times rank stay below 2^28 bytes)
+    const char* part = reinterpret_cast<const char*>(s.b + (static_cast<int64_t>(aid) * s.N + c.col0) * s.R);
+    const uint4 v = *reinterpret_cast<const uint4*>(part + static_cast<uint32_t>(2 * (col * s.R + (r0 < s.R ? r0 : 0))));
+    return whole ? v : first_of(v, rank - r0);
+  }
+  // Row r of the work-group's (below 2^8; strides are at most 2^23: 32-bit offsets in bytes).
+  static __device__ __forceinline__ Vec base(const bf16_t* rows, int64_t stride, const Cols& c, int r, int m) {
+    const int col = c.n0 + J * m < c.width ? c.n0 + J * m : 0;
+    return *reinterpret_cast<const Vec*>(reinterpret_cast<const char*>(rows) + offset(r, stride, col));
+  }
+  static __device__ __forceinline__ void store(bf16_t* rows, int64_t stride, const Cols& c, int r, int m, const Vec& v) {
+    *reinterpret_cast<Vec*>(reinterpret_cast<char*>(rows) + offset(r, stride, c.n0 + J * m)) = v;
+  }
+  static __device__ __forceinline__ uint32_t offset(int r, int64_t stride, int col) {
+    return 2 * (static_cast<uint32_t>(r) * static_cast<uint32_t>(stride) + static_cast<uint32_t>(col));
+  }
+  // base + scale * row i of the tiles' results
+  static __device__ __forceinline__ Vec add(const Vec& base, const f32x4_t (&acc)[J], int i, float scale) {
+    uint32_t w[J / 2];
+    __builtin_memcpy(w, &base, sizeof(w));
+#pragma unroll
+    for (int j = 0; j < J / 2; ++j)
+      w[j] = pack_bf16x2(fmaf(scale, acc[2 * j][i], lo_bf16(w[j])), fmaf(scale, acc[2 * j + 1][i], hi_bf16(w[j])));
+    Vec v;
+    __builtin_memcpy(&v, w, sizeof(w));
+    return v;
+  }
+};
+
+template <int J>
+__device__ __forceinline__ Cols cols_of(const Shape& s, int block, int wave) {
+  constexpr int kCols = 16 * J * kExpandWaves;
+  Cols c{0, 0, 0, 0};
+  for (; c.part < s.n_parts - 1; ++c.part) {
+    const int nb = (s.cols[c.part] + kCols - 1) / kCols;
     if (block < nb) break;
     block -= nb;
-    col0 += s.cols[part];
+    c.col0 += s.cols[c.part];
   }
-  const int width = s.cols[part];
-  const int n0 = (block * kExpandWaves + wave) * kWaveCols;  // in the part
-  if (n0 >= width) return;
+  c.width = s.cols[c.part];
+  c.n0 = block * kCols + wave * 16 * J;
+  return c;
+}
+
+template <int J>
+unsigned col_blocks(const Shape& s) {
+  unsigned n = 0;
+  for (int p = 0; p < s.n_parts; ++p) n += (s.cols[p] + 16 * J * kExpandWaves - 1) / (16 * J * kExpandWaves);
+  return n;
+}
+
+// Few rows: one group, 64 columns a wave.
+constexpr int kFewJ = 4;
+__global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_few_kernel(const Shape s) {
+  constexpr int J = kFewJ;
+  using O = Out<J>;
+  __shared__ int list[kTile];
+  __shared__ uint2 hs[128 / 16][kTile][2][4];  // [block of ranks][row][high, low][four ranks]
+  const int lane = threadIdx.x & 63;
+  const int m = lane & 15, g = lane >> 4;
+  const Cols cols = cols_of<J>(s, blockIdx.x, wave_id());
+  int aid = 0;
+  const int count = few_group(s, blockIdx.y, &aid, list);
   const bool in_place = s.base == s.out && s.base_stride == s.out_stride;
-  for (int t = 0; t < tiles; ++t) {
-    const int64_t row0 = (static_cast<int64_t>(blockIdx.y) * tiles + t) * kTile;
-    if (row0 >= s.rows) break;
-    const int n_rows = static_cast<int>(min<int64_t>(kTile, s.rows - row0));
-    const int id = tile_id(s, row0, lane);
-    const int64_t row = row0 + m;
-    for_groups(id, (1u << n_rows) - 1, few ? static_cast<int>(blockIdx.z) : -1, [&](int aid, unsigned mine) {
-      const bool has_row = (mine >> m) & 1;
-      const int n = n0 + 16 * g;  // the lane's 16 columns of row m
+  if (count == 0 || (aid < 0 && in_place)) return;
+  const bool has_col = cols.n0 + J * m < cols.width;
+  const bf16_t* base = s.base + cols.col0;
+  bf16_t* out = s.out + cols.col0;
+  // (rows past the group's are read as its last)
+  typename O::Vec bv[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bv[i] = O::base(base, s.base_stride, cols, list[min(4 * g + i, count - 1)], m);
+  if (aid < 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (has_col && 4 * g + i < count) O::store(out, s.out_stride, cols, list[4 * g + i], m, bv[i]);
+    return;
+  }
+  // the first block's weights, asked for before its rank is known
+  uint4 wv[J];
+#pragma unroll
+  for (int j = 0; j < J; ++j) wv[j] = O::weights(s, cols, aid, j, m, 8 * (g & 1), 0, true);
+  const int rank = rank_of(s, aid);
+  const float scale = s.scale ? s.scale[aid] : 1.f;
+  // H of the group: every slice's partial asked for before the first is added
+  const int64_t plane = s.rows * s.h_cols;
+  for (int e = threadIdx.x; e < kTile * 4 * s.rank_blocks; e += 64 * kExpandWaves) {
+    const int q = e & 3, row = (e >> 2) & 15, rb = e >> 6;
+    if (row < count) {
+      const float4* p = reinterpret_cast<const float4*>(s.part + list[row] * static_cast<int64_t>(s.h_cols) +
+                                                        (cols.part * s.rank_blocks + rb) * 16) + q;
+      float4 v[kFewSlices];
+#pragma unroll
+      for (int i = 0; i < kFewSlices; ++i) v[i] = i < s.slices ? p[i * plane / 4] : float4{0.f, 0.f, 0.f, 0.f};
+      float4 sum = v[0];
+#pragma unroll
+      for (int i = 1; i < kFewSlices; ++i) sum = sum + v[i];
+      store_split(reinterpret_cast<bf16_t*>(hs[rb][row]), q, sum);
+    }
+  }
+  __syncthreads();
+  f32x4_t acc[J] = {};
+  for (int rb = 0; 16 * rb < rank; ++rb) {
+    const uint4 hv = *reinterpret_cast<const uint4*>(&hs[rb][min(m, count - 1)][g >> 1][2 * (g & 1)]);
+    if (16 * rb + 16 > rank) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) wv[j] = first_of(wv[j], rank - 16 * rb - 8 * (g & 1));
+    }
+    uint4 next[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) next[j] = O::weights(s, cols, aid, j, m, 16 * (rb + 1) + 8 * (g & 1), 0, true);
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(hv), as_frag(wv[j]), acc[j], 0, 0, 0);
+#pragma unroll
+    for (int j = 0; j < J; ++j) wv[j] = next[j];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (has_col && 4 * g + i < count) O::store(out, s.out_stride, cols, list[4 * g + i], m, O::add(bv[i], acc, i, scale));
+}
+
+// Many rows: 64 columns a wave, a run of tiles of 16 rows one after another.  The next tile's
+// base and H are on their way while a tile is worked, and the weights of the first kKept
+// blocks of ranks stay in registers while the adapter stays.
+constexpr int kManyJ = 4;
+constexpr int kManyRun = 8;  // at most
+constexpr int kKept = 2;
+__global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(const Shape s) {
+  constexpr int J = kManyJ;
+  using O = Out<J>;
+  const int lane = threadIdx.x & 63;
+  const int m = lane & 15, g = lane >> 4;
+  const Cols cols = cols_of<J>(s, blockIdx.x, wave_id());
+  if (cols.n0 >= cols.width) return;
+  const bool in_place = s.base == s.out && s.base_stride == s.out_stride;
+  const bool has_col = cols.n0 + J * m < cols.width;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.y) * (16 * s.run);
+  const int n_rows = static_cast<int>(min<int64_t>(16 * s.run, s.rows - row0));
+  int ids[(16 * kManyRun + 63) / 64];
+#pragma unroll
+  for (int i = 0; i < (16 * kManyRun + 63) / 64; ++i) {
+    ids[i] = -1;
+    if (64 * i + lane < n_rows) ids[i] = adapter_of(s, row0 + 64 * i + lane);
+  }
+  const char* h0 = reinterpret_cast<const char*>(s.h + 2 * (row0 * s.h_cols + cols.part * s.rank_blocks * 16));
+  // Of H, 16 bytes: ranks 8 (g & 1) .. of block rb, the high (g < 2) or low parts.  Rows past
+  // the last are read as the last, other adapters' rows as they are: no result of theirs is used.
+  auto load_h = [&](int r, int rb) {
+    const uint32_t at = 4 * min(r, n_rows - 1) * s.h_cols + 64 * min(rb, s.rank_blocks - 1) + 16 * g;
+    return *reinterpret_cast<const uint4*>(h0 + at);
+  };
+  const bf16_t* base = s.base + row0 * s.base_stride + cols.col0;
+  bf16_t* out = s.out + row0 * s.out_stride + cols.col0;
+  struct Ahead {
+    typename O::Vec base[4];
+    uint4 h[kKept];
+  };
+  auto fetch = [&](int t, Ahead& a) {
+#pragma unroll
+    for (int k = 0; k < kKept; ++k) a.h[k] = load_h(16 * t + m, k);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a.base[i] = O::base(base, s.base_stride, cols, min(16 * t + 4 * g + i, n_rows - 1), m);
+  };
+  uint4 wv[kKept][J];
+  int kept = -1, rank = 0;
+  float scale = 0.f;
+  auto keep = [&](int aid) {
+    kept = aid;
+    rank = rank_of(s, aid);
+    scale = s.scale ? s.scale[aid] : 1.f;
+#pragma unroll
+    for (int k = 0; k < kKept; ++k)
+#pragma unroll
+      for (int j = 0; j < J; ++j) wv[k][j] = O::weights(s, cols, aid, j, m, 16 * k + 8 * (g & 1), rank, true);
+    if (rank < 16 * kKept) {
+#pragma unroll
+      for (int k = 0; k < kKept; ++k)
+#pragma unroll
+        for (int j = 0; j < J; ++j) wv[k][j] = first_of(wv[k][j], rank - 16 * k - 8 * (g & 1));
+    }
+  };
+  auto multiply = [&](const Ahead& a, int t, f32x4_t (&acc)[J]) {
+#pragma unroll
+    for (int k = 0; k < kKept; ++k)
+#pragma unroll
+      for (int j = 0; j < J && 16 * k < rank; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(a.h[k]), as_frag(wv[k][j]), acc[j], 0, 0, 0);
+    for (int rb = kKept; 16 * rb < rank; ++rb) {
+      const uint4 h = load_h(16 * t + m, rb);
+      uint4 w[J];
+#pragma unroll
+      for (int j = 0; j < J; ++j) w[j] = O::weights(s, cols, kept, j, m, 16 * rb + 8 * (g & 1), rank, true);
+      if (16 * rb + 16 > rank) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) w[j] = first_of(w[j], rank - 16 * rb - 8 * (g & 1));
+      }
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(h), as_frag(w[j]), acc[j], 0, 0, 0);
+    }
+  };
+  // The usual run, whole and of one adapter, in a loop without a condition on a load or
+  // store: each would make the next wait for all of them, stores included.
+  const int first = __builtin_amdgcn_readfirstlane(ids[0]);
+  bool same = n_rows == 16 * s.run && cols.n0 + 16 * J <= cols.width && first >= 0;
+#pragma unroll
+  for (int i = 0; i < (16 * kManyRun + 63) / 64; ++i) same &= __ballot(64 * i + lane < n_rows && ids[i] != first) == 0;
+  if (same) {
+    Ahead now, ahead;
+    fetch(0, ahead);
+    keep(first);
+    for (int t = 0; t < s.run; ++t) {
+      now = ahead;
+      fetch(t + 1, ahead);  // (of the last tile: the last row again)
+      f32x4_t acc[J] = {};
+      multiply(now, t, acc);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        O::store(out, s.out_stride, cols, 16 * t + 4 * g + i, m, O::add(now.base[i], acc, i, scale));
+    }
+    return;
+  }
+  for (int t = 0; 16 * t < n_rows; ++t) {
+    const int id = __shfl(ids[t / 4], 16 * (t % 4) + m);
+    Ahead now;
+    fetch(t, now);
+    for_adapters(id, (1ull << min(16, n_rows - 16 * t)) - 1, [&](int aid, unsigned long long mine) {
       if (aid < 0 && in_place) return;
-      uint4 bv[2] = {};
-      const bf16_t* bp = s.base + row * s.base_stride + col0 + n;
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (has_row && n + 8 * u < width) bv[u] = reinterpret_cast<const uint4*>(bp)[u];
-      f32x4_t acc[4] = {};
-      float scale = 0.f;
+      f32x4_t acc[J] = {};
       if (aid >= 0) {
-        scale = s.scale ? s.scale[aid] : 1.f;
-        const int rank = rank_of(s, aid);
-        const float* hp = s.h + row * s.h_cols + part * s.rank_blocks * 16;
-        const int64_t plane = s.rows * s.h_cols;
-        for (int rb = 0; 16 * rb < rank; ++rb) {
-          const int r0 = 16 * rb + 8 * (g & 1);
-          const int n_r = min(8, rank - r0);
-          float h[8] = {};
-          if (has_row && n_r > 0) {
-            for (int sl = 0; sl < s.slices; ++sl) {
-              const float4* p4 = reinterpret_cast<const float4*>(hp + sl * plane + r0);
-              const float4 u = p4[0], v = p4[1];
-              h[0] += u.x;
-              h[1] += u.y;
-              h[2] += u.z;
-              h[3] += u.w;
-              h[4] += v.x;
-              h[5] += v.y;
-              h[6] += v.z;
-              h[7] += v.w;
-            }
-          }
-          uint32_t w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            w[i] = pack_bf16x2(h[2 * i], h[2 * i + 1]);
-            if (g >= 2) {  // the low parts; none of a value that is not finite
-              const float l0 = h[2 * i] - lo_bf16(w[i]), l1 = h[2 * i + 1] - hi_bf16(w[i]);
-              w[i] = pack_bf16x2(isfinite(l0) ? l0 : 0.f, isfinite(l1) ? l1 : 0.f);
-            }
-          }
-          const uint4 hv = first_of(uint4{w[0], w[1], w[2], w[3]}, n_r);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            // tile j's row m is column 16 (m / 4) + 4 j + m % 4: a lane's four results of
-            // four tiles are 16 consecutive columns
-            const int col = n0 + 16 * (m >> 2) + 4 * j + (m & 3);
-            uint4 wv = uint4{0u, 0u, 0u, 0u};
-            if (col < width && n_r > 0)
-              wv = first_of(*reinterpret_cast<const uint4*>(
-                                s.b + (static_cast<int64_t>(aid) * s.N + col0 + col) * s.R + r0), n_r);
-            acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(wv), as_frag(hv), acc[j], 0, 0, 0);
-          }
-        }
+        if (aid != kept) keep(aid);
+        multiply(now, t, acc);
       }
-      if (!has_row) return;
-      bf16_t* op = s.out + row * s.out_stride + col0 + n;
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        if (n + 8 * u >= width) break;
-        if (aid < 0) {
-          reinterpret_cast<uint4*>(op)[u] = bv[u];
-          continue;
-        }
-        const uint32_t w[4] = {bv[u].x, bv[u].y, bv[u].z, bv[u].w};
-        uint32_t o[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x4_t& c = acc[2 * u + i / 2];
-          o[i] = pack_bf16x2(fmaf(scale, c[2 * (i & 1)], lo_bf16(w[i])), fmaf(scale, c[2 * (i & 1) + 1], hi_bf16(w[i])));
-        }
-        reinterpret_cast<uint4*>(op)[u] = uint4{o[0], o[1], o[2], o[3]};
-      }
+      for (int i = 0; i < 4; ++i)
+        if (has_col && ((mine >> (4 * g + i)) & 1))
+          O::store(out, s.out_stride, cols, 16 * t + 4 * g + i, m, aid < 0 ? now.base[i] : O::add(now.base[i], acc, i, scale));
     });
   }
 }
 
-Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows) {
+template <class C>
+unsigned h_groups(const Shape& s) {
+  return (s.h_cols / 16 + C::kCols - 1) / C::kCols;
+}
+
+// `rows` rows of the call from `first` on; *bytes: of the workspace they need.
+Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows, size_t* bytes) {
   Shape s{};
   s.x = static_cast<const bf16_t*>(c.x) + first * c.x_stride;
   s.base = static_cast<const bf16_t*>(c.base) + first * c.base_stride;
@@ -285,7 +551,6 @@ Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows) {
   s.b = static_cast<const bf16_t*>(c.b);
   s.scale = c.scale;
   s.ranks = c.ranks;
-  s.h = static_cast<float*>(c.workspace);
   s.rows = rows;
   s.x_stride = c.x_stride;
   s.base_stride = c.base_stride;
@@ -297,48 +562,64 @@ Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows) {
   for (int p = 0; p < c.n_parts; ++p) s.N += s.cols[p] = c.part_cols[p];
   s.rank_blocks = (s.R + 15) / 16;
   s.h_cols = 16 * s.n_parts * s.rank_blocks;
-  // K slices: few rows want more work-groups than there are tiles, many rows fill the chip by themselves.
-  const int64_t tiles = (s.rows + kTile - 1) / kTile;
-  const int64_t want = s.rows <= kFewRows ? 16 : 256 / std::max<int64_t>(1, tiles);
-  const int unit = 64 * kShrinkWaves;
-  const int most = (s.K + unit - 1) / unit;
-  const int n = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(want, most)));
-  s.k_slice = ((s.K + n - 1) / n + unit - 1) / unit * unit;
+  // K slices: enough work-groups for the chip
+  const bool few = rows <= kFewRows;
+  const int unit = 32 * (few ? FewShrink::kSteps * FewShrink::kWaves : ManyShrink::kSteps * ManyShrink::kWaves);
+  const int64_t most = (s.K + unit - 1) / unit;
+  const int64_t tiles = (rows + 16 * kManyTiles - 1) / (16 * kManyTiles) * h_groups<ManyShrink>(s);
+  const int64_t want = few ? kFewSlices : std::min<int64_t>(kManySlices, 256 / std::max<int64_t>(1, tiles));
+  const int64_t n = std::max<int64_t>(1, std::min(want, most));
+  s.k_slice = static_cast<int>(((s.K + n - 1) / n + unit - 1) / unit * unit);
   s.slices = (s.K + s.k_slice - 1) / s.k_slice;
+  const int64_t planes = few || s.slices > 1 ? s.slices : 0;
+  // runs as long as leave two work-groups for a CU
+  s.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kManyRun, (rows + 15) / 16 * col_blocks<kManyJ>(s) / 512)));
+  s.part = static_cast<float*>(c.workspace);
+  s.h = reinterpret_cast<bf16_t*>(s.part + planes * rows * s.h_cols);
+  *bytes = static_cast<size_t>((planes + (few ? 0 : 1)) * rows * s.h_cols) * sizeof(float);
   return s;
 }
 
 }  // namespace
 
-// Rows worked at once: grids stay below 2^32 threads (kMaxCols columns at 256 a work-group
-// of 256, four row tiles each).
-constexpr int64_t kRowsAtOnce = int64_t{1} << 17;
+// Rows worked at once: grids stay below 2^32 threads (at most 2^20 / 512 + 4 work-groups of 256
+// threads across, a 32nd of the rows down).
+constexpr int64_t kRowsAtOnce = int64_t{1} << 16;
 
 size_t adapter_workspace_bytes(const span_adapter_call& a) {
   size_t most = 0;
   // the last rows of a long call may be few, and split K further
   for (const int64_t n : {std::min(a.n_rows, kRowsAtOnce), a.n_rows % kRowsAtOnce}) {
-    const Shape s = shape_of(a, 0, n);
-    most = std::max(most, static_cast<size_t>(s.slices) * n * s.h_cols * sizeof(float));
+    size_t bytes = 0;
+    (void)shape_of(a, 0, n, &bytes);
+    most = std::max(most, bytes);
   }
   return most;
 }
 
 hipError_t launch_adapter_apply(const span_adapter_call& a, hipStream_t st) {
   for (int64_t first = 0; first < a.n_rows; first += kRowsAtOnce) {
-    const Shape s = shape_of(a, first, std::min(kRowsAtOnce, a.n_rows - first));
-    const bool few = s.rows <= kFewRows;
-    const unsigned tiles = static_cast<unsigned>((s.rows + kTile - 1) / kTile);
-    const unsigned groups = few ? static_cast<unsigned>(std::min<int64_t>(kTile, s.rows)) : 1;
-    const int col_groups = (s.h_cols / 16 + kGroupCols - 1) / kGroupCols;
-    adapter_shrink_kernel<<<dim3(s.slices * col_groups, tiles, groups), 64 * kShrinkWaves, 0, st>>>(s, few);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    unsigned blocks = 0;
-    for (int p = 0; p < s.n_parts; ++p)
-      blocks += (s.cols[p] + kExpandWaves * kWaveCols - 1) / (kExpandWaves * kWaveCols);
-    const unsigned per = few ? 1 : 4;
-    adapter_expand_kernel<<<dim3(blocks, (tiles + per - 1) / per, groups), 64 * kExpandWaves, 0, st>>>(s, few, per);
+    size_t bytes = 0;
+    const Shape s = shape_of(a, first, std::min(kRowsAtOnce, a.n_rows - first), &bytes);
+    hipError_t e = hipSuccess;
+    if (s.rows <= kFewRows) {
+      const unsigned rows = static_cast<unsigned>(s.rows);
+      adapter_shrink_kernel<true, FewShrink><<<dim3(s.slices * h_groups<FewShrink>(s), rows), 64 * FewShrink::kWaves, 0, st>>>(s);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      adapter_expand_few_kernel<<<dim3(col_blocks<kFewJ>(s), rows), 64 * kExpandWaves, 0, st>>>(s);
+    } else {
+      const unsigned tiles = static_cast<unsigned>((s.rows + 16 * kManyTiles - 1) / (16 * kManyTiles));
+      adapter_shrink_kernel<false, ManyShrink><<<dim3(s.slices * h_groups<ManyShrink>(s), tiles), 64 * ManyShrink::kWaves, 0, st>>>(s);
+      e = hipGetLastError();
+      if (e == hipSuccess && s.slices > 1) {
+        adapter_finish_kernel<<<static_cast<unsigned>((s.rows * s.h_cols / 4 + 255) / 256), 256, 0, st>>>(s);
+        e = hipGetLastError();
+      }
+      if (e != hipSuccess) return e;
+      const unsigned runs = static_cast<unsigned>((s.rows + 16 * s.run - 1) / (16 * s.run));
+      adapter_expand_many_kernel<<<dim3(col_blocks<kManyJ>(s), runs), 64 * kExpandWaves, 0, st>>>(s);
+    }
     e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

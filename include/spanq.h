@@ -340,6 +340,16 @@ int span_plan_decode(span_plan_t* plan, const int32_t* n_new, const int64_t* row
 int span_decode_attend(span_plan_t* plan, int32_t layer, const void* q, const void* k, const void* v, void* out,
                        void* stream);
 
+/* Take back the last n_drop[q] tokens that decode steps appended to query q's cross
+ * segment (drafted tokens that verification refused, span_verify_drafts): the next step
+ * appends at their positions, and pages that held nothing else are free again (a plan
+ * that takes them on another stream is ordered after this plan's work by the caller, as
+ * after span_plan_commit).  Call after the step's span_decode_attend for every layer:
+ * until the next span_plan_decode that returns SPAN_ESTATE.  The totals of span_stats
+ * keep what the steps appended.  SPAN_EINVAL (nothing changed) for more tokens than the
+ * steps appended and kept; SPAN_ESTATE before any step and after commit. */
+int span_plan_rewind(span_plan_t* plan, const int32_t* n_drop);
+
 /* ---------------------------------------------------------------- bulk scheduling */
 
 /* An execution order for a bulk of n_queries queries that clusters fragment reuse in
@@ -422,6 +432,45 @@ typedef struct {
 int span_model_create(span_pool* pool, const span_model_config* cfg, span_model** out);
 int span_model_destroy(span_model* model);
 
+/* Norms of the layers' queries and keys: before the attention calls, each head of q and k
+ * goes through RMSNorm with rms_eps and the layer's gain (span_qk_norm_rope without the
+ * rotation, which the attention calls make).  q_norm, k_norm: host tables of num_layers
+ * device pointers, bf16 [head_dim]; a table or an entry may be NULL (not normed).  The
+ * tables are copied, the gains must outlive the model.  Keys are cached normed: change
+ * them only with an empty pool. */
+int span_model_set_qk_norm(span_model* model, const void* const* q_norm, const void* const* k_norm);
+
+/* Low-rank adapters of the layers' projections (span_adapter_apply).  An adapter acts on a
+ * query's cross segment and on the tokens decoded after it, and on no prefix or fragment:
+ * their cached pages stay the same for every adapter, and shared.  Tables are host arrays of
+ * num_layers device pointers (bf16); a table or an entry may be NULL (that projection has
+ * none), a and b go together.  Parts: q|k|v three, o one, gate|up two, down one.  The tables
+ * are copied, the weights must outlive their use.  A projection's result is rounded to
+ * bf16, then the adapter's part added and rounded again. */
+typedef struct {
+  int32_t n_adapters;
+  int32_t max_rank;          /* multiple of 8, 8 .. 128 */
+  const float* scale;        /* device [n_adapters], NULL: 1 */
+  const int32_t* ranks;      /* device [n_adapters], NULL: max_rank */
+  const void* const* a_qkv;  /* [n_adapters][3][max_rank][hidden] */
+  const void* const* b_qkv;  /* [n_adapters][(num_q_heads + 2 num_kv_heads) head_dim][max_rank] */
+  const void* const* a_o;    /* [n_adapters][1][max_rank][num_q_heads head_dim] */
+  const void* const* b_o;    /* [n_adapters][hidden][max_rank] */
+  const void* const* a_gate_up;  /* [n_adapters][2][max_rank][hidden] */
+  const void* const* b_gate_up;  /* [n_adapters][2 ffn][max_rank] */
+  const void* const* a_down; /* [n_adapters][1][max_rank][ffn] */
+  const void* const* b_down; /* [n_adapters][hidden][max_rank] */
+} span_model_adapters;
+
+/* Give the model its adapters (NULL or n_adapters = 0: none). */
+int span_model_set_adapters(span_model* model, const span_model_adapters* adapters);
+
+/* The adapter of each of the plan's queries (host [n_queries], below 0: none; NULL: none at
+ * all) in the span_model_* calls on it from here on, which return SPAN_EINVAL for an id that the model does
+ * not have.  Set it before span_model_forward and leave it: the cross segment's keys and
+ * values are the adapter's. */
+int span_plan_set_adapters(span_plan_t* plan, const int32_t* adapters);
+
 /* Run the rows a plan computes (span_plan_rows: new prefix/fragment tokens, then
  * cross tokens) through the first n_layers layers, calling span_prefill_fragments
  * and span_cross_attend of `plan` per layer; cached rows are not computed, their
@@ -451,6 +500,32 @@ int span_model_forward(span_model* model, span_plan_t* plan, const int32_t* row_
  * model's own buffers hold the step's activations. */
 int span_model_decode(span_model* model, span_plan_t* plan, const int32_t* tokens, float* logits_out,
                       int32_t* next_tokens, void* stream);
+
+/* Random numbers and temperatures of a decode step with drafts (span_verify_drafts). */
+typedef struct {
+  const float* u_accept;     /* host [n_queries][max_drafts], in [0, 1) */
+  const float* u_sample;     /* host [n_queries], in [0, 1) */
+  const float* temperature;  /* host [n_queries], <= 0: greedy; NULL: all greedy, the numbers not read */
+  const float* draft_logits; /* device: the drafts' distributions, a row of [vocab] for every draft of every
+                                query that decodes, in order; NULL: drafts without a distribution */
+} span_sampling;
+
+/* A decode step that checks drafted tokens (speculative decoding; with no drafts, one
+ * that samples): every query q with tokens[q] >= 0 feeds that token and its n_drafts[q] drafts
+ * through the stack in one pass, the LM head gives the logits after each of them,
+ * span_verify_drafts keeps what it may and draws one more token, and span_plan_rewind takes
+ * the refused drafts back.  out_tokens (host [n_queries][max_drafts + 1]) receives the
+ * n_out[q] tokens that follow tokens[q]: the kept drafts, then the drawn one, which the next
+ * step feeds (n_out = 0, tokens -1, for a query that does not decode).
+ * - drafts: host [n_queries][max_drafts], 0 <= id < vocab; n_drafts: host [n_queries], 0 ..
+ *   max_drafts; both NULL with max_drafts = 0.  max_drafts at most SPAN_MAX_DRAFTS.
+ * - sampling: NULL: greedy, which gives the tokens of span_model_decode, but where the
+ *   GEMMs' rounding for another number of rows turns a near tie.
+ * - logprobs: optional host [n_queries][max_drafts + 1].
+ * Waits for the stream. */
+int span_model_decode_drafts(span_model* model, span_plan_t* plan, const int32_t* tokens, const int32_t* drafts,
+                             const int32_t* n_drafts, int32_t max_drafts, const span_sampling* sampling,
+                             int32_t* out_tokens, int32_t* n_out, float* logprobs, void* stream);
 
 /* ---------------------------------------------------------------- row operators */
 

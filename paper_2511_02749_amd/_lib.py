@@ -32,7 +32,8 @@ EXPORTS = [
     "span_probe_read_peak", "span_plan_static", "span_model_create", "span_model_destroy", "span_model_forward",
     "span_parse_serialized", "span_bulk_order", "span_plan_moves", "span_plan_decode", "span_decode_attend",
     "span_model_decode", "span_probe_gemm", "span_qk_norm_rope", "span_adapter_workspace", "span_adapter_apply",
-    "span_verify_workspace", "span_verify_drafts",
+    "span_verify_workspace", "span_verify_drafts", "span_plan_rewind", "span_plan_set_adapters",
+    "span_model_set_qk_norm", "span_model_set_adapters", "span_model_decode_drafts",
 ]
 SPAN_STATIC_SCRATCH_BYTES = 64 << 20
 SPAN_FLAG_TIMING = 1
@@ -109,6 +110,18 @@ class ModelConfig(ctypes.Structure):
                 ("final_norm", ctypes.c_void_p), ("lm_head", ctypes.c_void_p)]
 
 
+class ModelAdapters(ctypes.Structure):
+    _fields_ = [("n_adapters", ctypes.c_int32), ("max_rank", ctypes.c_int32), ("scale", ctypes.c_void_p),
+                ("ranks", ctypes.c_void_p)] + [(n, ctypes.POINTER(ctypes.c_void_p)) for n in
+                                               ("a_qkv", "b_qkv", "a_o", "b_o", "a_gate_up", "b_gate_up", "a_down",
+                                                "b_down")]
+
+
+class Sampling(ctypes.Structure):
+    _fields_ = [("u_accept", ctypes.POINTER(ctypes.c_float)), ("u_sample", ctypes.POINTER(ctypes.c_float)),
+                ("temperature", ctypes.POINTER(ctypes.c_float)), ("draft_logits", ctypes.c_void_p)]
+
+
 _LIB = None
 
 
@@ -162,6 +175,12 @@ def load():
         "span_probe_mfma_peak": (I32, [I32, I32, VP, P(ctypes.c_double)]),
         "span_probe_read_peak": (I32, [VP, ctypes.c_size_t, I32, VP, P(ctypes.c_double)]),
         "span_probe_gemm": (I32, [VP, VP, VP, I64, I64, I64, I32, I32, VP, P(I32), P(ctypes.c_double)]),
+        "span_plan_rewind": (I32, [VP, P(I32)]),
+        "span_plan_set_adapters": (I32, [VP, P(I32)]),
+        "span_model_set_qk_norm": (I32, [VP, P(VP), P(VP)]),
+        "span_model_set_adapters": (I32, [VP, P(ModelAdapters)]),
+        "span_model_decode_drafts": (I32, [VP, VP, P(I32), P(I32), P(I32), I32, P(Sampling), P(I32), P(I32),
+                                           P(ctypes.c_float), VP]),
         # argument records packed by row_ops.py
         "span_qk_norm_rope": (I32, [ctypes.c_char_p, VP]),
         "span_adapter_workspace": (I32, [ctypes.c_char_p, P(ctypes.c_size_t)]),
@@ -183,6 +202,19 @@ def _check(rc: int):
 
 def _i32p(a: np.ndarray):
     return a.ctypes.data_as(ctypes.POINTER(ctypes.c_int32))
+
+
+def _f32p(a: np.ndarray):
+    return a.ctypes.data_as(ctypes.POINTER(ctypes.c_float))
+
+
+def _table(seq, layers: int):
+    """A host table of `layers` device pointers (None: a null table)."""
+    if seq is None:
+        return None
+    if len(seq) != layers:
+        raise SpanError(SPAN_EINVAL, "a table needs an entry for each layer")
+    return (ctypes.c_void_p * layers)(*[_ptr(x) for x in seq])
 
 
 def _ptr(x) -> Optional[int]:
@@ -455,6 +487,24 @@ class Plan:
         _check(load().span_plan_decode(self._h, _i32p(n), r.ctypes.data_as(ctypes.POINTER(ctypes.c_int64)),
                                        _stream(stream) if stream is not None else self._stream))
 
+    def rewind(self, n_drop):
+        """Take back the last n_drop[q] tokens that decode steps appended (span_plan_rewind)."""
+        n = np.ascontiguousarray(n_drop, np.int32)
+        if n.shape != (self.n_queries,):
+            raise SpanError(SPAN_EINVAL, "rewind: one count for each query")
+        _check(load().span_plan_rewind(self._h, _i32p(n)))
+
+    def set_adapters(self, ids):
+        """The adapter of each query in the model's calls on this plan, below 0 or None: none
+        (span_plan_set_adapters)."""
+        if ids is None:
+            _check(load().span_plan_set_adapters(self._h, None))
+            return
+        a = np.ascontiguousarray([-1 if i is None else i for i in ids], np.int32)
+        if a.shape != (self.n_queries,):
+            raise SpanError(SPAN_EINVAL, "set_adapters: one id for each query")
+        _check(load().span_plan_set_adapters(self._h, _i32p(a)))
+
     def decode_attend(self, layer: int, q, k, v, out, stream=None):
         _check(load().span_decode_attend(self._h, layer, _ptr(q), _ptr(k), _ptr(v), _ptr(out),
                                          _stream(stream) if stream is not None else self._stream))
@@ -521,6 +571,75 @@ class Model:
                                          _i32p(toks) if toks is not None else None,
                                          _stream(stream) if stream is not None else plan._stream))
         return [int(t) for t in toks[: plan.n_queries]] if toks is not None else None
+
+    def set_qk_norm(self, q_norm=None, k_norm=None):
+        """Head norms of the layers' queries and keys (span_model_set_qk_norm): a gain [head_dim] for
+        each layer (None: not normed), or None for none."""
+        L = self.cfg.num_layers
+        _check(load().span_model_set_qk_norm(self._h, _table(q_norm, L), _table(k_norm, L)))
+        self._keep_norms = (q_norm, k_norm)
+
+    def set_adapters(self, n_adapters: int = 0, max_rank: int = 0, scale=None, ranks=None, qkv=None, o=None,
+                     gate_up=None, down=None):
+        """Low-rank adapters of the projections (span_model_set_adapters): each of qkv, o, gate_up,
+        down is None or a pair (a, b) of per-layer sequences of device tensors (an entry may be None),
+        a [n, parts, rank, in] and b [n, out, rank].  Without arguments: none."""
+        L = self.cfg.num_layers
+        cfg = ModelAdapters(n_adapters=n_adapters, max_rank=max_rank, scale=_ptr(scale), ranks=_ptr(ranks))
+        for name, pair in (("qkv", qkv), ("o", o), ("gate_up", gate_up), ("down", down)):
+            for side, seq in zip("ab", pair or (None, None)):
+                t = _table(seq, L)
+                if t is not None:
+                    setattr(cfg, f"{side}_{name}", ctypes.cast(t, ctypes.POINTER(ctypes.c_void_p)))
+        _check(load().span_model_set_adapters(self._h, ctypes.byref(cfg)))
+        self._keep_adapters = (scale, ranks, qkv, o, gate_up, down)
+
+    def decode_drafts(self, plan: "Plan", tokens, drafts=None, u_accept=None, u_sample=None, temperature=None,
+                      draft_logits=None, logprobs: bool = False, stream=None):
+        """A decode step that checks drafted tokens, or samples (span_model_decode_drafts): tokens[q] >= 0
+        and then drafts[q] are fed to query q.  Returns the tokens that follow for each query ([] where
+        tokens[q] < 0); with logprobs, (tokens, their log-probabilities).  temperature[q] > 0 needs
+        u_sample[q] and u_accept[q][..]; None: greedy.  draft_logits: device float32, a row for each draft
+        of the decoding queries in order, or None."""
+        n = plan.n_queries
+        t = np.ascontiguousarray(tokens, np.int32)
+        lists = [[]] * n if drafts is None else [list(d) for d in drafts]
+        if t.shape != (n,) or len(lists) != n:
+            raise SpanError(SPAN_EINVAL, "decode_drafts: one token and one draft list for each query")
+        k = max([len(d) for d in lists], default=0)
+        d, ua = np.zeros((max(1, n), max(1, k)), np.int32), np.zeros((max(1, n), max(1, k)), np.float32)
+        nd = np.zeros(max(1, n), np.int32)
+        for q, row in enumerate(lists):
+            d[q, :len(row)] = row
+            nd[q] = len(row)
+        sampling = None
+        if temperature is not None or draft_logits is not None:
+            heat = np.zeros(max(1, n), np.float32)
+            us = np.zeros(max(1, n), np.float32)
+            if temperature is not None:
+                heat[:n] = temperature
+                us[:n] = 0.0 if u_sample is None else u_sample
+                if u_sample is None and np.any(heat > 0):
+                    raise SpanError(SPAN_EINVAL, "decode_drafts: a temperature needs random numbers")
+                for q, row in enumerate(lists if u_accept is None else u_accept):
+                    if len(row) < len(lists[q]) or (u_accept is None and row and heat[q] > 0):
+                        raise SpanError(SPAN_EINVAL, "decode_drafts: a draft needs a random number")
+                    if u_accept is not None:
+                        ua[q, :nd[q]] = row[:nd[q]]
+            rows = int(sum(nd[q] for q in range(n) if t[q] >= 0))
+            if draft_logits is not None and (tuple(draft_logits.shape) != (rows, self.cfg.vocab) or
+                                             not draft_logits.is_contiguous() or draft_logits.dtype != torch.float32):
+                raise SpanError(SPAN_EINVAL, "decode_drafts: draft_logits must be float32 [drafts, vocab]")
+            sampling = ctypes.byref(Sampling(u_accept=_f32p(ua), u_sample=_f32p(us), temperature=_f32p(heat),
+                                             draft_logits=_ptr(draft_logits)))
+        out, n_out = np.zeros((max(1, n), k + 1), np.int32), np.zeros(max(1, n), np.int32)
+        lp = np.zeros((max(1, n), k + 1), np.float32)
+        _check(load().span_model_decode_drafts(self._h, plan._h, _i32p(t), _i32p(d) if k else None,
+                                               _i32p(nd) if k else None, k, sampling, _i32p(out), _i32p(n_out),
+                                               _f32p(lp) if logprobs else None,
+                                               _stream(stream) if stream is not None else plan._stream))
+        got = [[int(x) for x in out[q, :n_out[q]]] for q in range(n)]
+        return (got, [[float(x) for x in lp[q, :n_out[q]]] for q in range(n)]) if logprobs else got
 
     def decode(self, plan: "Plan", tokens, logits_out=None, stream=None):
         """One greedy decode step (span_model_decode): tokens[q] >= 0 is fed to query q;

@@ -7,6 +7,7 @@
 #include <cstdio>
 #include <cstdint>
 #include <cstring>
+#include <exception>
 #include <limits>
 #include <mutex>
 #include <new>
@@ -190,6 +191,8 @@ struct span_plan_t {
   hipEvent_t dec_ready = nullptr;   // recorded on dec_stream after the upload
   std::vector<hipEvent_t> dec_pending;
   bool decoding = false;            // decode steps planned: prefill and cross calls are over
+  bool rewound = false;             // the last step's tokens were taken back: its attention calls are over
+  std::vector<int32_t> adapters;    // per query (span_plan_set_adapters), empty: none
   std::vector<std::vector<hipEvent_t>> ev_decode;
 };
 
@@ -228,6 +231,18 @@ void spanq::plan_last_cross_rows(const span_plan_t* plan, std::vector<int64_t>* 
   for (const auto& ids : plan->plan.query_spans) {
     const SpanPlan& c = plan->plan.spans[ids.back()];
     rows->push_back(c.n_tok > 0 ? c.row + c.n_tok - 1 : -1);
+  }
+}
+
+const std::vector<int32_t>& spanq::plan_adapters(const span_plan_t* plan) { return plan->adapters; }
+
+void spanq::plan_cross_spans(const span_plan_t* plan, std::vector<int64_t>* row0, std::vector<int32_t>* n) {
+  row0->clear();
+  n->clear();
+  for (const auto& ids : plan->plan.query_spans) {
+    const SpanPlan& c = plan->plan.spans[ids.back()];
+    row0->push_back(c.row);
+    n->push_back(c.n_tok);
   }
 }
 
@@ -849,6 +864,7 @@ int span_plan_decode(span_plan_t* pl, const int32_t* n_new, const int64_t* rows,
   int rc = pool->index->decode(&P, n, r, t, &msg);
   if (rc) return fail(rc, "span_plan_decode: " + msg);
   pl->decoding = true;
+  pl->rewound = false;
   if (pool->cfg.device < 0) return SPAN_OK;
   hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = hipSetDevice(pool->cfg.device);
@@ -894,11 +910,43 @@ int span_plan_decode(span_plan_t* pl, const int32_t* n_new, const int64_t* rows,
   return SPAN_OK;
 }
 
+int span_plan_rewind(span_plan_t* pl, const int32_t* n_drop) {
+  if (!pl) return fail(SPAN_EINVAL, "span_plan_rewind: null plan");
+  if (pl->committed) return fail(SPAN_ESTATE, "span_plan_rewind: plan already committed");
+  if (!pl->decoding) return fail(SPAN_ESTATE, "span_plan_rewind: no decode step planned");
+  const size_t nq = pl->plan.query_spans.size();
+  if (nq > 0 && !n_drop) return fail(SPAN_EINVAL, "span_plan_rewind: null argument");
+  try {
+    std::string msg;
+    const int rc = pl->pool->index->rewind(&pl->plan, std::vector<int32_t>(n_drop, n_drop + nq), &msg);
+    if (rc) return fail(rc, "span_plan_rewind: " + msg);
+  } catch (const std::exception& e) {
+    return fail(SPAN_ENOMEM, std::string("span_plan_rewind: ") + e.what());
+  }
+  pl->rewound = true;
+  return SPAN_OK;
+}
+
+int span_plan_set_adapters(span_plan_t* pl, const int32_t* adapters) {
+  if (!pl) return fail(SPAN_EINVAL, "span_plan_set_adapters: null plan");
+  const size_t nq = pl->plan.query_spans.size();
+  std::vector<int32_t> ids;
+  try {
+    if (adapters) ids.assign(adapters, adapters + nq);
+  } catch (const std::exception& e) {
+    return fail(SPAN_ENOMEM, std::string("span_plan_set_adapters: ") + e.what());
+  }
+  for (int32_t& id : ids) id = std::max(id, -1);
+  if (std::all_of(ids.begin(), ids.end(), [](int32_t id) { return id < 0; })) ids.clear();
+  pl->adapters = std::move(ids);
+  return SPAN_OK;
+}
+
 int span_decode_attend(span_plan_t* pl, int32_t layer, const void* q, const void* k, const void* v, void* out,
                        void* stream) {
   int rc = attention_common(pl, layer, "span_decode_attend");
   if (rc) return rc;
-  if (!pl->dec.meta) return fail(SPAN_ESTATE, "span_decode_attend: no decode step planned");
+  if (!pl->dec.meta || pl->rewound) return fail(SPAN_ESTATE, "span_decode_attend: no decode step planned");
   const Plan::DecodeStep& d = pl->plan.dec;
   if (d.tokens == 0) return SPAN_OK;
   if (!q || !k || !v || !out) return fail(SPAN_EINVAL, "span_decode_attend: null activation pointer");

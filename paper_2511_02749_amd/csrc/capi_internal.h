@@ -36,4 +36,10 @@ void pool_shape(const span_pool* pool, int32_t out[5]);
 // Caller row of each query's last cross token, -1 for a query without one.
 void plan_last_cross_rows(const span_plan_t* plan, std::vector<int64_t>* rows);
 
+// The adapter of each query's cross and decoded rows (span_plan_set_adapters), -1 for none;
+// empty if the plan has none at all.  The cross rows of query q before any decode step
+// are caller rows row0[q] .. row0[q] + n[q] - 1.
+const std::vector<int32_t>& plan_adapters(const span_plan_t* plan);
+void plan_cross_spans(const span_plan_t* plan, std::vector<int64_t>* row0, std::vector<int32_t>* n);
+
 }  // namespace spanq

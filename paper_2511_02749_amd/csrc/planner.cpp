@@ -956,6 +956,8 @@ int PoolIndex::decode(Plan* p, const std::vector<int32_t>& n_new, const std::vec
            " free, " + std::to_string(n_evictable_) + " evictable";
     return SPAN_ENOMEM;
   }
+  p->decoded.resize(nq, 0);
+  p->stale_tail.resize(nq, 0);
   Plan::DecodeStep& d = p->dec;
   d = Plan::DecodeStep{};
   std::vector<CrossTile> ct;
@@ -982,9 +984,12 @@ int PoolIndex::decode(Plan* p, const std::vector<int32_t>& n_new, const std::vec
     const int32_t pos_first = cross.final0 + cur;
     for (int32_t i = 0; i < n;) {
       const int32_t pg = (cur + i) / ps, s0 = (cur + i) % ps, m = std::min(ps - s0, n - i);
-      d.writes.push_back(SlotWrite{cross.pages[pg], s0, m, static_cast<int32_t>(rows[q] + i), pos_first + i, {0, 0, 0}});
+      d.writes.push_back(SlotWrite{cross.pages[pg], s0, m, static_cast<int32_t>(rows[q] + i), pos_first + i,
+                                   s0 == 0 || p->stale_tail[q], {0, 0}});
       i += m;
     }
+    p->stale_tail[q] = 0;
+    p->decoded[q] += n;
     cross.n_tok = cur + n;
     p->max_pos = std::max(p->max_pos, cross.final0 + cross.n_tok);
     const int32_t kv0 = static_cast<int32_t>(d.kv.size());
@@ -1006,6 +1011,37 @@ int PoolIndex::decode(Plan* p, const std::vector<int32_t>& n_new, const std::vec
   p->decode_steps += 1;
   p->decode_tokens += total;
   p->decode_pages += d.pages_new;
+  return SPAN_OK;
+}
+
+int PoolIndex::rewind(Plan* p, const std::vector<int32_t>& n_drop, std::string* msg) {
+  const size_t nq = p->query_spans.size();
+  for (size_t q = 0; q < nq; ++q)
+    if (n_drop[q] < 0 || n_drop[q] > (q < p->decoded.size() ? p->decoded[q] : 0)) {
+      *msg = "only tokens of decode steps can be taken back";
+      return SPAN_EINVAL;
+    }
+  p->dec = Plan::DecodeStep{};
+  // the last of `ids` that is `pid` (pages go from the end, where they were added)
+  auto drop = [](std::vector<int32_t>& ids, int32_t pid) {
+    const auto it = std::find(ids.rbegin(), ids.rend(), pid);
+    if (it != ids.rend()) ids.erase(std::next(it).base());
+  };
+  for (size_t q = 0; q < nq; ++q) {
+    if (n_drop[q] == 0) continue;
+    SpanPlan& cross = p->spans[p->query_spans[q].back()];
+    cross.n_tok -= n_drop[q];
+    p->decoded[q] -= n_drop[q];
+    const size_t keep = static_cast<size_t>((cross.n_tok + page_size_ - 1) / page_size_);
+    while (cross.pages.size() > keep) {
+      const int32_t pid = cross.pages.back();
+      cross.pages.pop_back();
+      drop(p->new_pages, pid);
+      drop(p->cross_pages, pid);
+      push_free(pid);
+    }
+    p->stale_tail[q] = cross.n_tok % page_size_ != 0;
+  }
   return SPAN_OK;
 }
 

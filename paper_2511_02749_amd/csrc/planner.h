@@ -155,6 +155,10 @@ struct Plan {
     int64_t tokens = 0, pages_new = 0, pairs = 0;
   } dec;
   int64_t decode_steps = 0, decode_tokens = 0, decode_pages = 0;
+  // Per query (from the first decode step on): tokens the steps appended that were not
+  // taken back, and whether the last page holds tokens that were.
+  std::vector<int32_t> decoded;
+  std::vector<char> stale_tail;
 };
 
 class PoolIndex {
@@ -171,6 +175,9 @@ class PoolIndex {
   // work lists in p->dec.  Returns 0, -2 (pool full; plan and pool unchanged) or -1.
   int decode(Plan* p, const std::vector<int32_t>& n_new, const std::vector<int64_t>& rows, const Tiling& tiling,
              std::string* msg);
+  // Take back the last n_drop[q] decoded tokens of each query's cross segment and free
+  // the pages that held nothing else.  Returns 0 or -1 (nothing changed).
+  int rewind(Plan* p, const std::vector<int32_t>& n_drop, std::string* msg);
   void commit(Plan* p);
   void release(Plan* p);  // destroy without commit
   void reset();

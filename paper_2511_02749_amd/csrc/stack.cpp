@@ -16,11 +16,18 @@
 // over the chip, the rest on hipBLASLt.  Rows that hit the cache are never
 // computed: their keys and values are already in the pool's pages, which is the
 // point of the method (section 5.6).
+//
+// A model may norm the heads of q and k on their way to the attention calls, and add
+// low-rank adapters to the products of cross and decoded rows; both are row operators
+// (row_ops.h), and both take the place of the fused GEMV steps for few rows.  A decode
+// step with drafts runs several rows of a query and lets the verification operator
+// decide how many of them stay.
 #include <hip/hip_runtime.h>
 #include <hipblaslt/hipblaslt.h>
 
 #include <algorithm>
 #include <cstring>
+#include <exception>
 #include <new>
 #include <map>
 #include <string>
@@ -30,6 +37,7 @@
 
 #include "../../include/spanq.h"
 #include "capi_internal.h"
+#include "row_ops.h"
 #include "stack_kernels.h"
 
 using namespace spanq;
@@ -219,12 +227,85 @@ struct span_model {
   Buf q, k, v, o;
   // row lists, LM head
   Buf rows, toks, last, nf, part, logits, tok_out, best;
+  // head norms per layer (null: none)
+  std::vector<const void*> q_norm, k_norm;
+  // adapters of the four products (kQkv ..): per layer, null where a product has none
+  int n_adapters = 0, adapter_rank = 0;
+  const float* adapter_scale = nullptr;
+  const int32_t* adapter_ranks = nullptr;
+  std::vector<const void*> adapter_a[4], adapter_b[4];
+  Buf adapter_ids, adapter_ws;
+  // decode steps with drafts: logits of every row, verification's inputs, outputs and workspace
+  Buf vlogits, vin, vout, vws;
   int32_t* host_stage = nullptr;  // pinned staging of the row lists
   size_t host_stage_cap = 0;
   hipEvent_t staged = nullptr;     // the last upload from host_stage
 };
 
 namespace {
+
+enum { kQkv, kO, kGateUp, kDown };
+
+// Rows of a forward or decode call that have adapters: compact rows row0 .. row0 + n - 1, the
+// adapter of each (-1: none) in pinned memory; n = 0 when no row has one.
+struct AdaptedRows {
+  int64_t row0 = 0, n = 0;
+  const int32_t* ids = nullptr;
+};
+
+// One product's adapters over the adapted rows of x [T][K] and y [T][sum of the parts].
+span_adapter_call adapter_call(const span_model* m, int proj) {
+  const span_model_config& c = m->cfg;
+  span_adapter_call a{};
+  a.n_adapters = m->n_adapters;
+  a.max_rank = m->adapter_rank;
+  a.scale = m->adapter_scale;
+  a.ranks = m->adapter_ranks;
+  a.device = m->device;
+  a.n_parts = 1;
+  a.part_cols[0] = c.hidden;
+  if (proj == kQkv) {
+    a.in_features = c.hidden;
+    a.n_parts = 3;
+    a.part_cols[0] = c.num_q_heads * c.head_dim;
+    a.part_cols[1] = a.part_cols[2] = c.num_kv_heads * c.head_dim;
+  } else if (proj == kO) {
+    a.in_features = c.num_q_heads * c.head_dim;
+  } else if (proj == kGateUp) {
+    a.in_features = c.hidden;
+    a.n_parts = 2;
+    a.part_cols[0] = a.part_cols[1] = c.ffn;
+  } else {
+    a.in_features = c.ffn;
+  }
+  return a;
+}
+
+int add_adapter(span_model* m, int proj, int l, const AdaptedRows& ad, const void* x, void* y, hipStream_t s) {
+  if (ad.n == 0 || m->adapter_a[proj].empty() || !m->adapter_a[proj][l]) return SPAN_OK;
+  span_adapter_call a = adapter_call(m, proj);
+  int64_t cols = 0;
+  for (int p = 0; p < a.n_parts; ++p) cols += a.part_cols[p];
+  a.x = static_cast<const char*>(x) + ad.row0 * a.in_features * 2;
+  a.base = a.out = static_cast<char*>(y) + ad.row0 * cols * 2;
+  a.ids = m->adapter_ids.as<int32_t>();
+  a.a = m->adapter_a[proj][l];
+  a.b = m->adapter_b[proj][l];
+  a.workspace = m->adapter_ws.p;
+  a.workspace_bytes = m->adapter_ws.cap;
+  a.x_stride = a.in_features;
+  a.base_stride = a.out_stride = cols;
+  a.n_rows = ad.n;
+  return span_adapter_apply(&a, s);
+}
+
+// Does any of the plan's ids not exist, or does any exist at all?
+int check_adapters(const span_model* m, const std::vector<int32_t>& ids, const char* who) {
+  for (int32_t id : ids)
+    if (id >= m->n_adapters)
+      return report(SPAN_EINVAL, (std::string(who) + ": the plan names an adapter that the model does not have").c_str());
+  return SPAN_OK;
+}
 
 int check_config(span_pool* pool, const span_model_config* c) {
   if (!pool || !c) return report(SPAN_EINVAL, "span_model_create: null argument");
@@ -290,12 +371,18 @@ size_t skinny_scratch(const span_model_config& c, int64_t T) {
 // the row list (compact row i -> attention row), the tokens and the LM-head rows.
 // Buffers grow with the stream drained, so no launch still reads the old ones.
 int prepare(span_model* m, int64_t T, int64_t R, const int32_t* h_rows, const int32_t* h_toks, const int32_t* h_last,
-            int nh, hipStream_t s, const char* who) {
+            int nh, const AdaptedRows& ad, hipStream_t s, const char* who) {
   const span_model_config& c = m->cfg;
   const int H = c.hidden, hq = c.num_q_heads, hkv = c.num_kv_heads, d = c.head_dim, F = c.ffn, V = c.vocab;
   const int64_t qkv_w = static_cast<int64_t>(hq + 2 * hkv) * d;
   const size_t bf = 2;
   const size_t Tz = static_cast<size_t>(T), Rz = static_cast<size_t>(R);
+  size_t adapter_ws = 0;
+  for (int proj = kQkv; proj <= kDown && ad.n > 0; ++proj) {
+    span_adapter_call a = adapter_call(m, proj);
+    a.n_rows = ad.n;
+    adapter_ws = std::max(adapter_ws, adapter_workspace_bytes(a));
+  }
   struct Need {
     Buf* b;
     size_t bytes;
@@ -307,7 +394,9 @@ int prepare(span_model* m, int64_t T, int64_t R, const int32_t* h_rows, const in
       {&m->part, static_cast<size_t>(lm_head_chunks(H, V)) * 8 * V * 4}, {&m->logits, static_cast<size_t>(8) * V * 4},
       {&m->tok_out, 8 * 4}, {&m->best, argmax_scratch_bytes(8, V)},
       {&m->gemm.gemv_part, T <= 8 ? gemv_scratch(c, static_cast<int>(T)) : 0},
-      {&m->gemm.sk_part, skinny_scratch(c, T)}};
+      {&m->gemm.sk_part, skinny_scratch(c, T)},
+      {&m->adapter_ids, static_cast<size_t>(ad.n) * 4},
+      {&m->adapter_ws, adapter_ws}};
   bool grow = false;
   for (const Need& nd : needs) grow |= nd.bytes > nd.b->cap;
   hipError_t e = hipSuccess;
@@ -320,6 +409,8 @@ int prepare(span_model* m, int64_t T, int64_t R, const int32_t* h_rows, const in
   e = T > 0 ? hipMemcpyAsync(m->rows.p, h_rows, Tz * 4, hipMemcpyHostToDevice, s) : hipSuccess;
   if (e == hipSuccess && T > 0) e = hipMemcpyAsync(m->toks.p, h_toks, Tz * 4, hipMemcpyHostToDevice, s);
   if (e == hipSuccess && nh > 0) e = hipMemcpyAsync(m->last.p, h_last, static_cast<size_t>(nh) * 4, hipMemcpyHostToDevice, s);
+  if (e == hipSuccess && ad.n > 0)
+    e = hipMemcpyAsync(m->adapter_ids.p, ad.ids, static_cast<size_t>(ad.n) * 4, hipMemcpyHostToDevice, s);
   if (e == hipSuccess) e = hipEventRecord(m->staged, s);
   if (e != hipSuccess) return hip_err(e, std::string(who) + ": row lists");
   return SPAN_OK;
@@ -328,9 +419,10 @@ int prepare(span_model* m, int64_t T, int64_t R, const int32_t* h_rows, const in
 // Embeddings of the T compact rows, then n_layers decoder layers; attn(l) runs the
 // span attention of layer l on the q/k/v/o buffers.  base >= 0: compact row i is
 // attention row base + i for every i, so the output projection reads the attention
-// output in place instead of through a gather.
+// output in place instead of through a gather.  R: attention rows.
 template <class Attn>
-int run_layers(span_model* m, int64_t T, int n_layers, int64_t base, hipStream_t s, const char* who, Attn attn) {
+int run_layers(span_model* m, int64_t T, int n_layers, int64_t base, int64_t R, const AdaptedRows& ad, hipStream_t s,
+               const char* who, Attn attn) {
   const span_model_config& c = m->cfg;
   const int H = c.hidden, hq = c.num_q_heads, hkv = c.num_kv_heads, d = c.head_dim, F = c.ffn;
   const int64_t qkv_w = static_cast<int64_t>(hq + 2 * hkv) * d;
@@ -340,7 +432,9 @@ int run_layers(span_model* m, int64_t T, int n_layers, int64_t base, hipStream_t
   if (e != hipSuccess) return hip_err(e, w + ": embedding");
   // Up to 8 rows: every GEMM is a GEMV whose second pass also does the step after it
   // (q/k/v split, SwiGLU, the next RMSNorm), bit for bit the separate kernels' result.
-  const bool gv = m->gemm.gemv_layer(T, qkv_w, H, F, static_cast<int64_t>(hq) * d);
+  // Adapters and head norms come between a GEMV and that step, so they take the GEMMs' way.
+  const bool normed_heads = !m->q_norm.empty() || !m->k_norm.empty();
+  const bool gv = ad.n == 0 && !normed_heads && m->gemm.gemv_layer(T, qkv_w, H, F, static_cast<int64_t>(hq) * d);
   float* gp = m->gemm.gemv_part.as<float>();
   const size_t gcap = m->gemm.gemv_part.cap;
   const int Ti = static_cast<int>(T);
@@ -361,8 +455,36 @@ int run_layers(span_model* m, int64_t T, int n_layers, int64_t base, hipStream_t
       }
       rc = m->gemm.run(m->n.p, m->w_qkv[l], m->wt_qkv[l], m->qkv.p, T, qkv_w, H, false, s);
       if (rc) return rc;
-      e = launch_scatter_qkv(m->qkv.p, rows, T, hq * d, hkv * d, m->q.p, m->k.p, m->v.p, s);
-      if (e != hipSuccess) return hip_err(e, w + ": q/k/v scatter");
+      rc = add_adapter(m, kQkv, l, ad, m->n.p, m->qkv.p, s);
+      if (rc) return rc;
+      if (normed_heads && T > 0) {
+        span_qk_norm a{};
+        a.q = m->qkv.p;
+        a.k = m->qkv.as<char>() + static_cast<int64_t>(hq) * d * 2;
+        a.v = m->qkv.as<char>() + static_cast<int64_t>(hq + hkv) * d * 2;
+        a.q_out = m->q.p;
+        a.k_out = m->k.p;
+        a.v_out = m->v.p;
+        a.q_gain = m->q_norm.empty() ? nullptr : m->q_norm[l];
+        a.k_gain = m->k_norm.empty() ? nullptr : m->k_norm[l];
+        a.rows = rows;
+        a.q_stride = a.k_stride = a.v_stride = qkv_w;
+        a.q_out_stride = hq * d;
+        a.k_out_stride = a.v_out_stride = hkv * d;
+        a.n_rows = T;
+        a.out_rows = R;
+        a.num_q_heads = hq;
+        a.num_kv_heads = hkv;
+        a.head_dim = d;
+        a.dtype = SPAN_BF16;
+        a.device = m->device;
+        a.eps = c.rms_eps;
+        rc = span_qk_norm_rope(&a, s);
+        if (rc) return rc;
+      } else {
+        e = launch_scatter_qkv(m->qkv.p, rows, T, hq * d, hkv * d, m->q.p, m->k.p, m->v.p, s);
+        if (e != hipSuccess) return hip_err(e, w + ": q/k/v scatter");
+      }
     }
     rc = attn(l);
     if (rc) return rc;
@@ -390,18 +512,23 @@ int run_layers(span_model* m, int64_t T, int n_layers, int64_t base, hipStream_t
       continue;
     }
     rc = m->gemm.run(oc, m->w_o[l], m->wt_o[l], m->x.p, T, H, static_cast<int64_t>(hq) * d, true, s);
+    if (!rc) rc = add_adapter(m, kO, l, ad, oc, m->x.p, s);
     if (rc) return rc;
     e = launch_rmsnorm(m->x.p, nullptr, m->ffn_norm[l], m->n.p, T, H, c.rms_eps, s);
     if (e != hipSuccess) return hip_err(e, w + ": ffn norm");
     rc = m->gemm.run(m->n.p, m->w_gate_up[l], m->wt_gate_up[l], m->gu.p, T, 2 * static_cast<int64_t>(F), H, false, s);
+    if (!rc) rc = add_adapter(m, kGateUp, l, ad, m->n.p, m->gu.p, s);
     if (rc) return rc;
     e = launch_swiglu(m->gu.p, m->act.p, T, F, s);
     if (e != hipSuccess) return hip_err(e, w + ": swiglu");
-    if (l + 1 < n_layers) {
+    const bool adapted_down = ad.n > 0 && !m->adapter_a[kDown].empty() && m->adapter_a[kDown][l];
+    if (l + 1 < n_layers && !adapted_down) {
       rc = m->gemm.run_norm(m->act.p, m->w_down[l], m->wt_down[l], m->x.p, T, H, F, m->attn_norm[l + 1], m->n.p,
                             c.rms_eps, &normed, s);
     } else {
       rc = m->gemm.run(m->act.p, m->w_down[l], m->wt_down[l], m->x.p, T, H, F, true, s);
+      if (!rc) rc = add_adapter(m, kDown, l, ad, m->act.p, m->x.p, s);
+      normed = false;
     }
     if (rc) return rc;
   }
@@ -519,7 +646,8 @@ int span_model_destroy(span_model* m) {
   m->gemm.destroy();
   m->wt_buf.release();
   for (Buf* b : {&m->x, &m->n, &m->qkv, &m->oc, &m->gu, &m->act, &m->q, &m->k, &m->v, &m->o, &m->rows, &m->toks,
-                 &m->last, &m->nf, &m->part, &m->logits, &m->tok_out, &m->best})
+                 &m->last, &m->nf, &m->part, &m->logits, &m->tok_out, &m->best, &m->adapter_ids, &m->adapter_ws,
+                 &m->vlogits, &m->vin, &m->vout, &m->vws})
     b->release();
   if (m->host_stage) (void)hipHostFree(m->host_stage);
   if (m->staged) (void)hipEventDestroy(m->staged);
@@ -555,11 +683,15 @@ int span_model_forward(span_model* m, span_plan_t* plan, const int32_t* row_toke
   std::unordered_map<int64_t, int32_t> last_at;
   for (int64_t r : last_rows)
     if (r >= 0) last_at.emplace(r, -1);
+  const std::vector<int32_t>& adapters = plan_adapters(plan);
+  rc = check_adapters(m, adapters, "span_model_forward");
+  if (rc) return rc;
   int32_t* h_rows = nullptr;
-  rc = stage_area(m, 2 * static_cast<size_t>(T) + static_cast<size_t>(nq) + 8, &h_rows, "span_model_forward");
+  rc = stage_area(m, 3 * static_cast<size_t>(T) + static_cast<size_t>(nq) + 8, &h_rows, "span_model_forward");
   if (rc) return rc;
   int32_t* h_toks = h_rows + T;
   int32_t* h_last = h_toks + T;
+  int32_t* h_ids = h_last + nq;
   for (int64_t i = 0; i < T; ++i) {
     const int64_t r = rows64[static_cast<size_t>(i)];
     if (r < 0 || r >= n_rows) return report(SPAN_EINVAL, "span_model_forward: a planned row lies outside row_tokens");
@@ -579,12 +711,27 @@ int span_model_forward(span_model* m, span_plan_t* plan, const int32_t* row_toke
       q_of.push_back(qi);
     }
   const int nh = static_cast<int>(q_of.size());
+  AdaptedRows ad;
+  if (!adapters.empty() && n_cross > 0) {
+    // cross rows alone: prefix and fragment rows are cached for every adapter
+    std::vector<int64_t> row0;
+    std::vector<int32_t> n;
+    plan_cross_spans(plan, &row0, &n);
+    std::unordered_map<int64_t, int32_t> id_of;
+    for (int qi = 0; qi < nq; ++qi)
+      for (int32_t j = 0; j < n[qi]; ++j) id_of[row0[qi] + j] = adapters[qi];
+    for (int64_t i = n_pre; i < T; ++i) {
+      const auto it = id_of.find(h_rows[i]);
+      h_ids[i - n_pre] = it != id_of.end() ? it->second : -1;
+    }
+    ad = AdaptedRows{n_pre, n_cross, h_ids};
+  }
   int64_t base = T > 0 ? h_rows[0] : -1;
   for (int64_t i = 1; i < T && base >= 0; ++i)
     if (h_rows[i] != base + i) base = -1;
-  rc = prepare(m, T, n_rows, h_rows, h_toks, h_last, nh, s, "span_model_forward");
+  rc = prepare(m, T, n_rows, h_rows, h_toks, h_last, nh, ad, s, "span_model_forward");
   if (rc) return rc;
-  rc = run_layers(m, T, n_layers, base, s, "span_model_forward", [&](int l) {
+  rc = run_layers(m, T, n_layers, base, n_rows, ad, s, "span_model_forward", [&](int l) {
     int r = span_prefill_fragments(plan, l, m->q.p, m->k.p, m->v.p, m->o.p, s);
     if (!r) r = span_cross_attend(plan, l, m->q.p, m->k.p, m->v.p, m->o.p, s);
     return r;
@@ -632,22 +779,28 @@ int span_model_decode(span_model* m, span_plan_t* plan, const int32_t* tokens, f
     for (int qi = 0; qi < nq; ++qi) next_tokens[qi] = -1;
   const int nd = static_cast<int>(q_of.size());
   if (nd == 0) return SPAN_OK;
-  int rc = span_plan_decode(plan, n_new.data(), rows.data(), s);
+  const std::vector<int32_t>& adapters = plan_adapters(plan);
+  int rc = check_adapters(m, adapters, "span_model_decode");
+  if (!rc) rc = span_plan_decode(plan, n_new.data(), rows.data(), s);
   if (rc) return rc;
   // one compact row per decoding query; its attention row is the same index
   int32_t* h_rows = nullptr;
-  rc = stage_area(m, 3 * static_cast<size_t>(nd) + 8, &h_rows, "span_model_decode");
+  rc = stage_area(m, 4 * static_cast<size_t>(nd) + 8, &h_rows, "span_model_decode");
   if (rc) return rc;
   int32_t* h_toks = h_rows + nd;
   int32_t* h_last = h_toks + nd;
+  int32_t* h_ids = h_last + nd;
+  AdaptedRows ad;
   for (int i = 0; i < nd; ++i) {
     h_rows[i] = i;
     h_toks[i] = tokens[q_of[i]];
     h_last[i] = i;
+    if (!adapters.empty()) h_ids[i] = adapters[q_of[i]];
   }
-  rc = prepare(m, nd, nd, h_rows, h_toks, h_last, nd, s, "span_model_decode");
+  if (!adapters.empty()) ad = AdaptedRows{0, nd, h_ids};
+  rc = prepare(m, nd, nd, h_rows, h_toks, h_last, nd, ad, s, "span_model_decode");
   if (rc) return rc;
-  rc = run_layers(m, nd, c.num_layers, 0, s, "span_model_decode",
+  rc = run_layers(m, nd, c.num_layers, 0, nd, ad, s, "span_model_decode",
                   [&](int l) { return span_decode_attend(plan, l, m->q.p, m->k.p, m->v.p, m->o.p, s); });
   if (rc) return rc;
   if (!next_tokens && !logits_out) return SPAN_OK;
@@ -657,6 +810,256 @@ int span_model_decode(span_model* m, span_plan_t* plan, const int32_t* tokens, f
   if (next_tokens)
     for (int i = 0; i < nd; ++i) next_tokens[q_of[i]] = toks[i];
   return SPAN_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Fills a layer table from a caller's (null: empty).
+void take_table(const void* const* t, int layers, std::vector<const void*>* to) {
+  to->clear();
+  if (t) to->assign(t, t + layers);
+  if (std::all_of(to->begin(), to->end(), [](const void* p) { return !p; })) to->clear();
+}
+
+int set_qk_norm(span_model* m, const void* const* q_norm, const void* const* k_norm) {
+  for (const void* const* t : {q_norm, k_norm})
+    for (int l = 0; t && l < m->cfg.num_layers; ++l)
+      if (reinterpret_cast<uintptr_t>(t[l]) % 16 != 0)
+        return report(SPAN_EINVAL, "span_model_set_qk_norm: gains must be 16-byte aligned");
+  take_table(q_norm, m->cfg.num_layers, &m->q_norm);
+  take_table(k_norm, m->cfg.num_layers, &m->k_norm);
+  return SPAN_OK;
+}
+
+int set_adapters(span_model* m, const span_model_adapters* a) {
+  const int L = m->cfg.num_layers;
+  const int n = a ? a->n_adapters : 0;
+  if (n < 0 || (n > 0 && (a->max_rank < 8 || a->max_rank % 8 != 0 || a->max_rank > 128)))
+    return report(SPAN_EINVAL, "span_model_set_adapters: bad adapter count or rank (a multiple of 8 in [8, 128])");
+  const void* const* at[4] = {};
+  const void* const* bt[4] = {};
+  if (n > 0) {
+    const void* const* as[4] = {a->a_qkv, a->a_o, a->a_gate_up, a->a_down};
+    const void* const* bs[4] = {a->b_qkv, a->b_o, a->b_gate_up, a->b_down};
+    for (int p = 0; p < 4; ++p) {
+      at[p] = as[p];
+      bt[p] = bs[p];
+      bool ok = !at[p] == !bt[p];
+      for (int l = 0; ok && at[p] && l < L; ++l)
+        ok = !at[p][l] == !bt[p][l] && reinterpret_cast<uintptr_t>(at[p][l]) % 16 == 0 &&
+             reinterpret_cast<uintptr_t>(bt[p][l]) % 16 == 0;
+      if (!ok) return report(SPAN_EINVAL, "span_model_set_adapters: a and b go together, 16-byte aligned");
+    }
+  }
+  for (int p = 0; p < 4; ++p) {
+    take_table(at[p], L, &m->adapter_a[p]);
+    take_table(bt[p], L, &m->adapter_b[p]);
+  }
+  m->n_adapters = n;
+  m->adapter_rank = n > 0 ? a->max_rank : 0;
+  m->adapter_scale = n > 0 ? a->scale : nullptr;
+  m->adapter_ranks = n > 0 ? a->ranks : nullptr;
+  return SPAN_OK;
+}
+
+int decode_drafts(span_model* m, span_plan_t* plan, const int32_t* tokens, const int32_t* drafts,
+                  const int32_t* n_drafts, int32_t k, const span_sampling* sampling, int32_t* out_tokens,
+                  int32_t* n_out, float* logprobs, hipStream_t s) {
+  const char* who = "span_model_decode_drafts";
+  auto bad = [&](const char* what) { return report(SPAN_EINVAL, (std::string(who) + ": " + what).c_str()); };
+  if (plan_pool(plan) != m->pool) return bad("the plan belongs to another pool");
+  const span_model_config& c = m->cfg;
+  std::vector<int64_t> last_rows;
+  plan_last_cross_rows(plan, &last_rows);
+  const int nq = static_cast<int>(last_rows.size());
+  if (k < 0 || k > SPAN_MAX_DRAFTS) return bad("max_drafts must lie in [0, SPAN_MAX_DRAFTS]");
+  if (nq > 0 && (!tokens || !out_tokens || !n_out || (k > 0 && (!drafts || !n_drafts)))) return bad("null argument");
+  const bool warm = sampling && sampling->temperature;
+  if (nq > 0 && warm && (!sampling->u_sample || (k > 0 && !sampling->u_accept))) return bad("temperatures need random numbers");
+  std::vector<int> q_of;  // decoding queries, in order
+  std::vector<int32_t> n_new(static_cast<size_t>(nq), 0);
+  std::vector<int64_t> rows(static_cast<size_t>(nq), 0);
+  int64_t T = 0;
+  for (int qi = 0; qi < nq; ++qi) {
+    if (tokens[qi] < 0) continue;
+    const int32_t n = k > 0 ? n_drafts[qi] : 0;
+    if (n < 0 || n > k) return bad("n_drafts must lie in [0, max_drafts]");
+    bool ok = tokens[qi] < c.vocab;
+    for (int32_t j = 0; ok && j < n; ++j) {
+      const int32_t d = drafts[static_cast<int64_t>(qi) * k + j];
+      ok = d >= 0 && d < c.vocab;
+    }
+    if (!ok) return bad("token id outside the vocabulary");
+    n_new[qi] = 1 + n;
+    rows[qi] = T;
+    T += 1 + n;
+    q_of.push_back(qi);
+  }
+  const std::vector<int32_t>& adapters = plan_adapters(plan);
+  int rc = check_adapters(m, adapters, who);
+  if (rc) return rc;
+  const int64_t k1 = static_cast<int64_t>(k) + 1;
+  for (int64_t i = 0; i < nq * k1; ++i) {
+    out_tokens[i] = -1;
+    if (logprobs) logprobs[i] = 0.f;
+  }
+  for (int qi = 0; qi < nq; ++qi) n_out[qi] = 0;
+  const int nd = static_cast<int>(q_of.size());
+  if (nd == 0) return SPAN_OK;
+  hipError_t e = hipSetDevice(m->device);
+  if (e != hipSuccess) return hip_err(e, std::string(who) + ": hipSetDevice");
+  rc = span_plan_decode(plan, n_new.data(), rows.data(), s);
+  if (rc) return rc;
+  // a step that fails leaves the plan as it was
+  struct TakeBack {
+    span_plan_t* plan;
+    const std::vector<int32_t>& n;
+    bool armed = true;
+    ~TakeBack() {
+      if (!armed) return;
+      const std::string why = span_last_error();
+      (void)span_plan_rewind(plan, n.data());
+      (void)report(SPAN_EHIP, why.c_str());
+    }
+  } take_back{plan, n_new};
+  // staging: the row lists, then verification's inputs (drafts, u_accept: [nd][k]; n_drafts,
+  // first rows, u_sample, temperature: [nd])
+  const int64_t n_in = nd * (2 * static_cast<int64_t>(k) + 5);
+  int32_t* h_rows = nullptr;
+  rc = stage_area(m, static_cast<size_t>(4 * T + n_in), &h_rows, who);
+  if (rc) return rc;
+  int32_t* h_toks = h_rows + T;
+  int32_t* h_last = h_toks + T;
+  int32_t* h_ids = h_last + T;
+  int32_t* in = h_ids + T;
+  int32_t* in_drafts = in;
+  float* in_ua = reinterpret_cast<float*>(in_drafts + static_cast<int64_t>(nd) * k);
+  int32_t* in_n = reinterpret_cast<int32_t*>(in_ua + static_cast<int64_t>(nd) * k);
+  int32_t* in_row0 = in_n + nd;
+  int32_t* in_drow0 = in_row0 + nd;
+  float* in_us = reinterpret_cast<float*>(in_drow0 + nd);
+  float* in_heat = in_us + nd;
+  int64_t at = 0;
+  for (int i = 0; i < nd; ++i) {
+    const int qi = q_of[i];
+    const int32_t n = n_new[qi] - 1;
+    in_n[i] = n;
+    in_row0[i] = static_cast<int32_t>(at);
+    in_drow0[i] = static_cast<int32_t>(at - i);
+    in_us[i] = warm ? sampling->u_sample[qi] : 0.f;
+    in_heat[i] = warm ? sampling->temperature[qi] : 0.f;
+    for (int32_t j = 0; j < k; ++j) {
+      const int64_t from = static_cast<int64_t>(qi) * k + j, to = static_cast<int64_t>(i) * k + j;
+      in_drafts[to] = j < n ? drafts[from] : 0;
+      in_ua[to] = warm && j < n ? sampling->u_accept[from] : 0.f;
+    }
+    for (int32_t j = 0; j <= n; ++j, ++at) {
+      h_rows[at] = h_last[at] = static_cast<int32_t>(at);
+      h_toks[at] = j == 0 ? tokens[qi] : drafts[static_cast<int64_t>(qi) * k + j - 1];
+      h_ids[at] = adapters.empty() ? -1 : adapters[qi];
+    }
+  }
+  AdaptedRows ad;
+  if (!adapters.empty()) ad = AdaptedRows{0, T, h_ids};
+  // buffers of the verification (grown with the stream drained, as prepare's)
+  const size_t out_words = static_cast<size_t>(nd) * (1 + 2 * k1);
+  struct Need {
+    Buf* b;
+    size_t bytes;
+  } needs[] = {{&m->vlogits, static_cast<size_t>(T) * c.vocab * 4}, {&m->vin, static_cast<size_t>(n_in) * 4},
+               {&m->vout, out_words * 4}, {&m->vws, verify_workspace_bytes(nd, k, c.vocab)}};
+  for (const Need& need : needs)
+    if (need.bytes > need.b->cap) {
+      e = hipStreamSynchronize(s);
+      if (e == hipSuccess) e = need.b->ensure(need.bytes);
+      if (e != hipSuccess) return hip_err(e, std::string(who) + ": verification buffers");
+    }
+  rc = prepare(m, T, T, h_rows, h_toks, h_last, static_cast<int>(T), ad, s, who);
+  if (rc) return rc;
+  e = hipMemcpyAsync(m->vin.p, in, static_cast<size_t>(n_in) * 4, hipMemcpyHostToDevice, s);
+  if (e == hipSuccess) e = hipEventRecord(m->staged, s);
+  if (e != hipSuccess) return hip_err(e, std::string(who) + ": verification inputs");
+  rc = run_layers(m, T, c.num_layers, 0, T, ad, s, who,
+                  [&](int l) { return span_decode_attend(plan, l, m->q.p, m->k.p, m->v.p, m->o.p, s); });
+  if (rc) return rc;
+  rc = lm_head(m, static_cast<int>(T), m->vlogits.as<float>(), nullptr, s, who);
+  if (rc) return rc;
+  span_verify_call v{};
+  const int32_t* din = m->vin.as<int32_t>();
+  v.target_logits = m->vlogits.as<float>();
+  v.draft_logits = sampling ? sampling->draft_logits : nullptr;
+  v.target_row0 = din + (in_row0 - in);
+  v.draft_row0 = din + (in_drow0 - in);
+  v.drafts = din;
+  v.n_drafts = din + (in_n - in);
+  v.u_accept = reinterpret_cast<const float*>(din + static_cast<int64_t>(nd) * k);
+  v.u_sample = reinterpret_cast<const float*>(din + (in_drow0 - in) + nd);
+  v.temperature = v.u_sample + nd;
+  v.accepted = m->vout.as<int32_t>();
+  v.tokens = v.accepted + nd;
+  v.logprobs = reinterpret_cast<float*>(v.tokens + nd * k1);
+  v.workspace = m->vws.p;
+  v.workspace_bytes = m->vws.cap;
+  v.target_stride = v.draft_stride = c.vocab;
+  v.target_rows = T;
+  v.draft_rows = T - nd;
+  v.n_requests = nd;
+  v.max_drafts = k;
+  v.vocab = c.vocab;
+  v.device = m->device;
+  rc = span_verify_drafts(&v, s);
+  if (rc) return rc;
+  std::vector<int32_t> out(out_words);
+  e = hipMemcpyAsync(out.data(), m->vout.p, out_words * 4, hipMemcpyDeviceToHost, s);
+  if (e == hipSuccess) e = hipStreamSynchronize(s);
+  if (e != hipSuccess) return hip_err(e, std::string(who) + ": tokens");
+  std::vector<int32_t> drop(static_cast<size_t>(nq), 0);
+  take_back.armed = false;
+  for (int i = 0; i < nd; ++i) {
+    const int qi = q_of[i];
+    n_out[qi] = out[i] + 1;
+    drop[qi] = in_n[i] - out[i];
+    const int32_t* t = out.data() + nd + i * k1;
+    std::copy(t, t + k1, out_tokens + qi * k1);
+    if (logprobs) std::memcpy(logprobs + qi * k1, out.data() + nd + (nd + i) * k1, static_cast<size_t>(k1) * 4);
+  }
+  return span_plan_rewind(plan, drop.data());
+}
+
+// No C++ exception leaves the C entries: what they throw is a failed allocation.
+template <class F>
+int no_throw(const char* who, F f) {
+  try {
+    return f();
+  } catch (const std::exception& e) {
+    return report(SPAN_ENOMEM, (std::string(who) + ": " + e.what()).c_str());
+  }
+}
+
+}  // namespace
+
+extern "C" {
+
+int span_model_set_qk_norm(span_model* m, const void* const* q_norm, const void* const* k_norm) {
+  if (!m) return report(SPAN_EINVAL, "span_model_set_qk_norm: null model");
+  return no_throw("span_model_set_qk_norm", [&] { return set_qk_norm(m, q_norm, k_norm); });
+}
+
+int span_model_set_adapters(span_model* m, const span_model_adapters* adapters) {
+  if (!m) return report(SPAN_EINVAL, "span_model_set_adapters: null model");
+  return no_throw("span_model_set_adapters", [&] { return set_adapters(m, adapters); });
+}
+
+int span_model_decode_drafts(span_model* m, span_plan_t* plan, const int32_t* tokens, const int32_t* drafts,
+                             const int32_t* n_drafts, int32_t max_drafts, const span_sampling* sampling,
+                             int32_t* out_tokens, int32_t* n_out, float* logprobs, void* stream) {
+  if (!m || !plan) return report(SPAN_EINVAL, "span_model_decode_drafts: null argument");
+  return no_throw("span_model_decode_drafts", [&] {
+    return decode_drafts(m, plan, tokens, drafts, n_drafts, max_drafts, sampling, out_tokens, n_out, logprobs,
+                         static_cast<hipStream_t>(stream));
+  });
 }
 
 int span_probe_gemm(const void* x, const void* w, void* y, int64_t M, int64_t N, int64_t K, int32_t residual,

@@ -50,14 +50,16 @@ struct MovePage {
 
 // Decoded tokens to write into a page: slots slot0 .. slot0 + n - 1 from caller rows
 // src_row .., keys rotated at positions pos0 ..; the page's other slots are left as
-// they are.
+// they are, but for those past the tokens of a fresh write, which it zeroes: the page
+// comes from the free list, or holds tokens that were taken back.
 struct SlotWrite {
   int32_t page_id;
   int32_t slot0;
   int32_t n;
   int32_t src_row;
   int32_t pos0;
-  int32_t pad[3];
+  int32_t fresh;
+  int32_t pad[2];
 };
 
 // A tile of up to BM consecutive query rows of one span, against the key pages

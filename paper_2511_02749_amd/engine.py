@@ -1,4 +1,4 @@
-"""Greedy execution of span queries on a pool and a decoder stack.
+"""Execution of span queries on a pool and a decoder stack.
 
 The generate callbacks that ``spanquery.expand_generates`` takes, backed by the
 library: a batch of lowered span queries is laid out in one row space, planned
@@ -8,11 +8,17 @@ token (``span_model_forward``), then decoded greedily one token per step
 prefixes and fragments it computed stay cached for the queries after it.  Every
 step of the path runs in the native library; this module only lays out rows and
 loops over steps.
+
+With n_drafts > 0 a step feeds, after a query's last token, the tokens that followed the
+latest earlier place in its own tokens where the same few tokens stand (an answer over
+retrieved documents copies from them), and keeps those that the stack would have
+generated (``span_model_decode_drafts``).  With temperature > 0 tokens are sampled, from
+random numbers of `seed`.
 """
 from __future__ import annotations
 
 from dataclasses import dataclass, field
-from typing import List, Sequence
+from typing import List, Optional, Sequence
 
 import numpy as np
 
@@ -27,6 +33,20 @@ class CallStats:
     tokens_hit: int
     tokens_new: int
     decode_steps: int
+    drafts_fed: int = 0
+    drafts_kept: int = 0
+
+
+def lookup_drafts(tokens: Sequence[int], n: int, longest: int = 3) -> List[int]:
+    """Up to n tokens that followed the latest earlier place of the last tokens: of the last
+    `longest`, else of fewer, down to one; [] if even that stands nowhere else."""
+    toks = list(tokens)
+    for m in range(min(longest, len(toks) - 1), 0, -1):
+        tail = toks[-m:]
+        for at in range(len(toks) - m - 1, -1, -1):
+            if toks[at:at + m] == tail:
+                return toks[at + m:at + m + n]
+    return []
 
 
 @dataclass
@@ -35,35 +55,89 @@ class Engine:
     model: object                      # paper_2511_02749_amd.Model on that pool
     stream: object = None
     calls: List[CallStats] = field(default_factory=list)
+    n_drafts: int = 0                  # drafted tokens that a decode step checks, 0: none
+    temperature: float = 0.0           # 0: greedy
+    seed: int = 0
 
-    def generate_many(self, spans: Sequence[sq.Spans], max_tokens: int) -> List[List[int]]:
-        """Up to max_tokens greedy tokens for each query (one plan, one batch).  Every
-        query needs a cross segment: its first token is read at the last cross row."""
+    def __post_init__(self):
+        self._rng = np.random.default_rng(self.seed)
+
+    def generate_many(self, spans: Sequence[sq.Spans], max_tokens: int,
+                      adapters: Optional[Sequence[Optional[int]]] = None) -> List[List[int]]:
+        """Up to max_tokens tokens for each query (one plan, one batch), through the model's
+        adapter adapters[q] if given.  Every query needs a cross segment: its first token is
+        read at the last cross row."""
         if max_tokens < 1:
             raise ValueError("max_tokens must be at least 1")
-        queries, rows, at = [], [], 0
+        queries, rows, at, history = [], [], 0, []
         for sp in spans:
             if not sp.cross:
                 raise ValueError("a generate needs a cross segment to read its first token at")
             queries.append(sq.to_query(sp, row0=at))
             toks = list(sp.prefix) + [t for f in sp.fragments for t in f] + list(sp.cross)
             rows.extend(toks)
+            history.append(toks)
             at += len(toks)
         plan = self.pool.plan(queries, self.stream)
+        fed = kept = 0
         try:
-            cur = self.model.forward(plan, np.asarray(rows, np.int32), stream=self.stream)
+            if adapters is not None:
+                plan.set_adapters(adapters)
+            rows = np.asarray(rows, np.int32)
+            if self.temperature > 0:
+                cur = self._sample_first(plan, rows, len(queries))
+            else:
+                cur = self.model.forward(plan, rows, stream=self.stream)
             out = [[t] for t in cur]
-            for _ in range(max_tokens - 1):
-                cur = self.model.decode(plan, cur, stream=self.stream)
-                for o, t in zip(out, cur):
-                    o.append(t)
+            if self.n_drafts == 0 and not self.temperature > 0:
+                for _ in range(max_tokens - 1):
+                    cur = self.model.decode(plan, cur, stream=self.stream)
+                    for o, t in zip(out, cur):
+                        o.append(t)
+            else:
+                fed, kept = self._decode_checked(plan, history, out, max_tokens)
             st = plan.stats()
             self.calls.append(CallStats(queries=len(queries), pages_hit=st["pages_hit"], tokens_hit=st["tokens_hit"],
-                                        tokens_new=st["tokens_new"], decode_steps=st["decode_steps"]))
+                                        tokens_new=st["tokens_new"], decode_steps=st["decode_steps"],
+                                        drafts_fed=fed, drafts_kept=kept))
             plan.commit()
         finally:
             plan.destroy()
         return out
+
+    def _sample_first(self, plan, rows, n: int) -> List[int]:
+        import torch
+
+        from .row_ops import verify_drafts
+        dev = torch.device("cuda", self.pool.cfg.device)
+        stream = torch.cuda.ExternalStream(self.stream, dev) if isinstance(self.stream, int) and self.stream else \
+            self.stream or torch.cuda.current_stream(dev)
+        with torch.cuda.stream(stream):
+            logits = torch.empty((n, self.model.cfg.vocab), dtype=torch.float32, device=dev)
+            self.model.forward(plan, rows, logits_out=logits, first_tokens=False, stream=stream)
+            tokens = torch.empty((n, 1), dtype=torch.int32, device=dev)
+            verify_drafts(logits, None, None, torch.from_numpy(self._rng.random(n, np.float32)).to(dev),
+                          torch.full((n,), self.temperature, device=dev), torch.empty(n, dtype=torch.int32, device=dev),
+                          tokens)
+            return tokens[:, 0].tolist()
+
+    def _decode_checked(self, plan, history, out, max_tokens: int):
+        """Steps of drafts and sampled tokens until every query has max_tokens; (drafts fed, kept)."""
+        n, fed, kept = len(out), 0, 0
+        while any(len(o) < max_tokens for o in out):
+            open_ = [len(o) < max_tokens for o in out]
+            drafts = [lookup_drafts(h + o, min(self.n_drafts, max_tokens - len(o) - 1)) if go else []
+                      for h, o, go in zip(history, out, open_)]
+            got = self.model.decode_drafts(
+                plan, [o[-1] if go else -1 for o, go in zip(out, open_)], drafts,
+                u_accept=[self._rng.random(len(d), np.float32) for d in drafts],
+                u_sample=self._rng.random(n, np.float32), temperature=np.full(n, self.temperature, np.float32),
+                stream=self.stream)
+            fed += sum(len(d) for d in drafts)
+            kept += sum(len(g) - 1 for g in got if g)
+            for o, g in zip(out, got):
+                o.extend(g)
+        return fed, kept
 
     def generate(self, tokens: Sequence[int], max_tokens: int) -> List[int]:
         """A generate over plain messages: the tokens are the cross segment."""

@@ -595,7 +595,8 @@ typedef struct {
                            does not count and may hold anything */
   void* workspace;    /* span_adapter_workspace bytes, 16-byte aligned */
   size_t workspace_bytes;
-  int64_t x_stride, base_stride, out_stride; /* multiples of 8; rows 16-byte aligned, as a and b */
+  int64_t x_stride, base_stride, out_stride; /* multiples of 8, the last two at most 2^23; rows 16-byte
+                                                aligned, as a and b */
   int64_t n_rows;     /* below 2^31 */
   int32_t in_features; /* multiple of 8, at most 2^20 */
   int32_t n_adapters;

@@ -30,6 +30,7 @@ bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % 
 
 constexpr int64_t kMaxRows = std::numeric_limits<int32_t>::max();
 constexpr int64_t kMaxWide = int64_t{1} << 20;  // features, columns and requests
+constexpr int64_t kMaxStride = int64_t{1} << 23;  // of base and out: a work-group's rows in 32 bits
 
 // One of q, k, v: its input, output, strides and gain.
 const char* check_part(const void* in, const void* out, const void* gain, int64_t in_stride, int64_t out_stride,
@@ -119,8 +120,8 @@ int span_adapter_apply(const span_adapter_call* args, void* stream) {
       !aligned(a.workspace, 16))
     return bad(who, "rows, weights and workspace must be 16-byte aligned");
   if (a.x_stride < a.in_features || a.base_stride < n || a.out_stride < n || a.x_stride % 8 != 0 ||
-      a.base_stride % 8 != 0 || a.out_stride % 8 != 0)
-    return bad(who, "strides must be multiples of 8 and hold a row");
+      a.base_stride % 8 != 0 || a.out_stride % 8 != 0 || a.base_stride > kMaxStride || a.out_stride > kMaxStride)
+    return bad(who, "strides must be multiples of 8 and hold a row, base's and out's at most 2^23");
   if (a.base == a.out && a.base_stride != a.out_stride) return bad(who, "in place needs the same stride");
   if (a.workspace_bytes < adapter_workspace_bytes(a) || !a.workspace)
     return bad(who, "the workspace is smaller than span_adapter_workspace says");

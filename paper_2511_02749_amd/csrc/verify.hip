@@ -234,8 +234,9 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(const Args a) {
   }
 }
 
-// A row's largest logit, its lowest id (greedy requests) and its sum of weights, by one wave.
-__device__ __forceinline__ Stat whole_row(const Stat* st, int chunks, const Request& r, int lane) {
+// A row's largest logit, its lowest id (greedy requests) and its sum of weights, by one wave;
+// *own: what the lane's chunk, the lane-th, adds to that sum.
+__device__ __forceinline__ Stat whole_row(const Stat* st, int chunks, const Request& r, int lane, double* own) {
   Stat mine{0.0, -INFINITY, INT32_MAX};
   if (lane < chunks) mine = st[lane];
   float best = mine.max;
@@ -248,7 +249,7 @@ __device__ __forceinline__ Stat whole_row(const Stat* st, int chunks, const Requ
       if (st[i].max == best) arg = min(arg, st[i].arg);
     arg = wave_min(arg);
   }
-  double sum = mine.sum * weight(mine.max, best, r.c);
+  double sum = *own = mine.sum * weight(mine.max, best, r.c);
   for (int i = lane + 64; i < chunks; i += 64) sum += st[i].sum * weight(st[i].max, best, r.c);
   return Stat{wave_sum(sum), best, arg};
 }
@@ -257,13 +258,15 @@ __device__ __forceinline__ Stat whole_row(const Stat* st, int chunks, const Requ
 struct Verdict {
   Stat p[kMaxDrafts + 1], q[kMaxDrafts];
   float x[kMaxDrafts];  // the drafted tokens' logits
-  int keep[kMaxDrafts];
+  int d[kMaxDrafts], keep[kMaxDrafts];
 };
 
 // Acceptance of a request's drafts, by all waves of the work-group; returns the number
-// kept.  p and q of `v` hold the rows' sums afterwards.
+// kept.  p and q of `v` hold the rows' sums afterwards, chunk[j][i] (if given) what chunk i < 64
+// adds to target row j's.
 template <int kNW>
-__device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Verdict& v) {
+__device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Verdict& v,
+                                      double (*chunk)[64] = nullptr) {
   const span_verify_call& c = a.c;
   const int k = c.max_drafts;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -285,8 +288,10 @@ __device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Ve
     const int j = of_p ? e : e - r.n_drafts - 1;
     const Stat* st = of_p ? a.target + (static_cast<int64_t>(q) * (k + 1) + j) * a.chunks
                           : a.draft + (static_cast<int64_t>(q) * k + j) * a.chunks;
-    const Stat s = whole_row(st, a.chunks, r, lane);
+    double own;
+    const Stat s = whole_row(st, a.chunks, r, lane, &own);
     if (lane == 0) (of_p ? v.p[j] : v.q[j]) = s;
+    if (chunk && of_p) chunk[j][lane] = own;
   }
   __syncthreads();
   if (mine < r.n_drafts) {
@@ -301,6 +306,7 @@ __device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Ve
       keep = static_cast<double>(u) * qd < pd;
     }
     v.keep[j] = keep;
+    v.d[j] = d;
     v.x[j] = x;
   }
   __syncthreads();
@@ -340,7 +346,7 @@ __device__ __forceinline__ Left left_of(const Args& a, int q, const Request& r, 
       l.qm = v.q[n].max;
       l.qs = inverse(v.q[n].sum);
     } else {
-      const int d = c.drafts[static_cast<int64_t>(q) * c.max_drafts + n];
+      const int d = v.d[n];
       l.one_hot = d >= 0 && d < c.vocab ? d : -1;
     }
   }
@@ -375,8 +381,10 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
   constexpr int kPickWaves = kPickThreads / 64;
   constexpr int kEach = kChunk / kPickThreads;
   __shared__ Verdict v;
+  __shared__ double s_chunk[kMaxDrafts + 1][64];
   __shared__ double s_wave[kPickWaves];
   __shared__ int s_first, s_last;
+  __shared__ float s_x;
   const span_verify_call& c = a.c;
   const int q = a.q0 + static_cast<int>(blockIdx.x);
   const int k = c.max_drafts;
@@ -397,7 +405,7 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
     s_last = -1;
   }
   const float u_sample = c.u_sample[q];
-  const int n = accept<kPickWaves>(a, q, r, v);  // (its barriers also publish s_first and s_last)
+  const int n = accept<kPickWaves>(a, q, r, v, s_chunk);  // (its barriers also publish s_first and s_last)
   int token = -1;
   if (!(v.p[n].sum > 0.0)) {
   } else if (r.greedy) {
@@ -414,8 +422,8 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
       auto chunk_sum = [&](int i) -> double {
         if (i >= a.chunks) return 0.0;
         if (l.y) return a.left[static_cast<int64_t>(q) * a.chunks + i];
-        double s = st[i].sum * weight(st[i].max, l.pm, l.c) * l.ps;
-        if (l.one_hot >= 0 && l.one_hot / kChunk == i) s -= weight(l.x[l.one_hot], l.pm, l.c) * l.ps;
+        double s = (i < 64 ? s_chunk[n][i] : st[i].sum * weight(st[i].max, l.pm, l.c)) * l.ps;
+        if (l.one_hot >= 0 && l.one_hot / kChunk == i) s -= weight(v.x[n], l.pm, l.c) * l.ps;
         return s > 0.0 ? s : 0.0;
       };
       const double own = chunk_sum(lane);  // all of them up to 64 chunks
@@ -439,11 +447,17 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
     }
     // the token in the chunk: each thread tokens that follow one another
     const int i0 = chunk * kChunk + static_cast<int>(threadIdx.x) * kEach;
+    float x[kEach], y[kEach];
     double w[kEach], mine = 0.0;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      const bool in = i0 + e < c.vocab;
-      w[e] = in ? l.of(i0 + e, l.x[i0 + e], l.y ? l.y[i0 + e] : 0.f) : 0.0;
+      const int i = min(i0 + e, c.vocab - 1);
+      x[e] = l.x[i];
+      y[e] = l.y ? l.y[i] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      w[e] = i0 + e < c.vocab ? l.of(i0 + e, x[e], y[e]) : 0.0;
       mine += w[e];
     }
     const double upto = wave_scan(mine);
@@ -464,15 +478,19 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
     if (last >= 0) atomicMax(&s_last, last);
     __syncthreads();
     token = s_first != INT32_MAX ? s_first : s_last;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e)
+      if (i0 + e == token) s_x = x[e];
+    __syncthreads();
   }
   const int j = static_cast<int>(threadIdx.x);
   if (j <= k) {
-    const int t = j < n ? c.drafts[static_cast<int64_t>(q) * k + j] : j == n ? token : -1;
+    const int t = j < n ? v.d[j] : j == n ? token : -1;
     tokens[j] = t;
     if (lps) {
       float lp = 0.f;
       if (t >= 0) {
-        const float x = j < n ? v.x[j] : c.target_logits[(r.target_row + j) * c.target_stride + t];
+        const float x = j < n ? v.x[j] : r.greedy ? v.p[n].max : s_x;
         // the largest logit (an infinite one too) has no difference to scale
         const double d = x == v.p[j].max ? 0.0 : (static_cast<double>(x) - static_cast<double>(v.p[j].max)) * r.c;
         lp = static_cast<float>(d * 0.69314718055994530942 - log(v.p[j].sum));

@@ -62,7 +62,8 @@ def test_qk_norm_rope_refuses(lib, change):
     dict(c1=-8), dict(c0=1 << 20), dict(n_adapters=-1), dict(device=-1), dict(reserved=1), dict(x=0), dict(base=0),
     dict(out=0), dict(ids=0), dict(a=0), dict(b=0), dict(x=P + 8), dict(base=P + 2), dict(out=P + 4), dict(a=P + 8),
     dict(b=P + 8), dict(workspace=P + 4), dict(workspace=0), dict(workspace_bytes=0), dict(x_stride=56),
-    dict(x_stride=68), dict(base_stride=56), dict(out_stride=60), dict(out=P, out_stride=72),
+    dict(x_stride=68), dict(base_stride=56), dict(out_stride=60),
+    dict(base_stride=(1 << 23) + 8), dict(out_stride=(1 << 23) + 8), dict(out=P, out_stride=72),
 ])
 def test_adapter_apply_refuses(lib, change):
     _refused(lib, "span_adapter_apply", R._ADAPTER_REC, {**ADAPT, **change})

@@ -24,7 +24,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "dev_common.h"
 #include "mfma_common.h"
@@ -41,12 +40,13 @@ constexpr int kTile = 16;      // rows of a group, ranks of a block
 constexpr int kFewRows = 256;  // up to here the rows are grouped by adapter
 constexpr int kFewSlices = 8;  // work-groups over K for few rows, whose partials expand adds up
 constexpr int kManySlices = 16;
+constexpr int kManyGroups = 4;
 constexpr int kManyTiles = 4;  // 16-row tiles of a many-row work-group
 
 // Shrink work-groups: waves (each with its own part of K), 16-row and 16-column tiles of H,
 // and products of 32 values whose loads are in flight together.
 struct FewShrink {
-  static constexpr int kWaves = 8, kRows = 1, kCols = 1, kSteps = 4;
+  static constexpr int kWaves = 2, kRows = 1, kCols = 1, kSteps = 8;
 };
 struct ManyShrink {
   static constexpr int kWaves = 4, kRows = kManyTiles, kCols = 4, kSteps = 2;
@@ -244,8 +244,12 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
     const int64_t row0 = static_cast<int64_t>(blockIdx.y) * (16 * C::kRows);
     const int64_t row = row0 + lane;
     const unsigned long long live = __ballot(row < s.rows);
+    // the tile's adapters are dealt to kManyGroups work-groups: where a tile holds the end of one
+    // request and the start of the next, neither waits for the other
+    int n = 0;
     for_adapters(adapter_of(s, row), live, [&](int aid, unsigned long long mine) {
-      if (aid >= 0) work(aid, mine, [&](int i) -> int64_t { return row0 + i; });
+      if (aid >= 0 && n++ % kManyGroups == static_cast<int>(blockIdx.z))
+        work(aid, mine, [&](int i) -> int64_t { return row0 + i; });
     });
   }
 }
@@ -285,9 +289,11 @@ struct Cols {
 
 // J tiles of 16 columns: column m of tile j is column J m + j of the wave's, so that a lane's
 // results are J columns that follow one another.
-template <int J>
+// kStream: base and out pass the caches by (a call of many rows reads and writes each of
+// their lines once: 2048 rows of 28672 columns 79 -> 74 us).
+template <int J, bool kStream>
 struct Out {
-  using Vec = std::conditional_t<J == 8, uint4, uint2>;
+  typedef uint32_t Vec __attribute__((ext_vector_type(J / 2)));
   // Ranks r0 .. r0 + 7 of tile j's weights, those past `rank` zero.  Columns past the part's
   // and ranks past R are read as its first ones: no result of theirs is used.
   static __device__ __forceinline__ uint4 weights(const Shape& s, const Cols& c, int aid, int j, int m, int r0,
@@ -301,23 +307,25 @@ struct Out {
   // Row r of the work-group's (below 2^8; strides are at most 2^23: 32-bit offsets in bytes).
   static __device__ __forceinline__ Vec base(const bf16_t* rows, int64_t stride, const Cols& c, int r, int m) {
     const int col = c.n0 + J * m < c.width ? c.n0 + J * m : 0;
-    return *reinterpret_cast<const Vec*>(reinterpret_cast<const char*>(rows) + offset(r, stride, col));
+    const Vec* p = reinterpret_cast<const Vec*>(reinterpret_cast<const char*>(rows) + offset(r, stride, col));
+    return kStream ? __builtin_nontemporal_load(p) : *p;
   }
   static __device__ __forceinline__ void store(bf16_t* rows, int64_t stride, const Cols& c, int r, int m, const Vec& v) {
-    *reinterpret_cast<Vec*>(reinterpret_cast<char*>(rows) + offset(r, stride, c.n0 + J * m)) = v;
+    Vec* p = reinterpret_cast<Vec*>(reinterpret_cast<char*>(rows) + offset(r, stride, c.n0 + J * m));
+    if (kStream)
+      __builtin_nontemporal_store(v, p);
+    else
+      *p = v;
   }
   static __device__ __forceinline__ uint32_t offset(int r, int64_t stride, int col) {
     return 2 * (static_cast<uint32_t>(r) * static_cast<uint32_t>(stride) + static_cast<uint32_t>(col));
   }
   // base + scale * row i of the tiles' results
   static __device__ __forceinline__ Vec add(const Vec& base, const f32x4_t (&acc)[J], int i, float scale) {
-    uint32_t w[J / 2];
-    __builtin_memcpy(w, &base, sizeof(w));
+    Vec v;
 #pragma unroll
     for (int j = 0; j < J / 2; ++j)
-      w[j] = pack_bf16x2(fmaf(scale, acc[2 * j][i], lo_bf16(w[j])), fmaf(scale, acc[2 * j + 1][i], hi_bf16(w[j])));
-    Vec v;
-    __builtin_memcpy(&v, w, sizeof(w));
+      v[j] = pack_bf16x2(fmaf(scale, acc[2 * j][i], lo_bf16(base[j])), fmaf(scale, acc[2 * j + 1][i], hi_bf16(base[j])));
     return v;
   }
 };
@@ -348,7 +356,7 @@ unsigned col_blocks(const Shape& s) {
 constexpr int kFewJ = 4;
 __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_few_kernel(const Shape s) {
   constexpr int J = kFewJ;
-  using O = Out<J>;
+  using O = Out<J, false>;
   __shared__ int list[kTile];
   __shared__ uint2 hs[128 / 16][kTile][2][4];  // [block of ranks][row][high, low][four ranks]
   const int lane = threadIdx.x & 63;
@@ -423,7 +431,7 @@ constexpr int kManyRun = 8;  // at most
 constexpr int kKept = 2;
 __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(const Shape s) {
   constexpr int J = kManyJ;
-  using O = Out<J>;
+  using O = Out<J, true>;
   const int lane = threadIdx.x & 63;
   const int m = lane & 15, g = lane >> 4;
   const Cols cols = cols_of<J>(s, blockIdx.x, wave_id());
@@ -610,7 +618,7 @@ hipError_t launch_adapter_apply(const span_adapter_call& a, hipStream_t st) {
       adapter_expand_few_kernel<<<dim3(col_blocks<kFewJ>(s), rows), 64 * kExpandWaves, 0, st>>>(s);
     } else {
       const unsigned tiles = static_cast<unsigned>((s.rows + 16 * kManyTiles - 1) / (16 * kManyTiles));
-      adapter_shrink_kernel<false, ManyShrink><<<dim3(s.slices * h_groups<ManyShrink>(s), tiles), 64 * ManyShrink::kWaves, 0, st>>>(s);
+      adapter_shrink_kernel<false, ManyShrink><<<dim3(s.slices * h_groups<ManyShrink>(s), tiles, kManyGroups), 64 * ManyShrink::kWaves, 0, st>>>(s);
       e = hipGetLastError();
       if (e == hipSuccess && s.slices > 1) {
         adapter_finish_kernel<<<static_cast<unsigned>((s.rows * s.h_cols / 4 + 255) / 256), 256, 0, st>>>(s);

@@ -281,8 +281,12 @@ span_adapter_call adapter_call(const span_model* m, int proj) {
   return a;
 }
 
+bool has_adapter(const span_model* m, int proj, int l, const AdaptedRows& ad) {
+  return ad.n > 0 && !m->adapter_a[proj].empty() && m->adapter_a[proj][l];
+}
+
 int add_adapter(span_model* m, int proj, int l, const AdaptedRows& ad, const void* x, void* y, hipStream_t s) {
-  if (ad.n == 0 || m->adapter_a[proj].empty() || !m->adapter_a[proj][l]) return SPAN_OK;
+  if (!has_adapter(m, proj, l, ad)) return SPAN_OK;
   span_adapter_call a = adapter_call(m, proj);
   int64_t cols = 0;
   for (int p = 0; p < a.n_parts; ++p) cols += a.part_cols[p];
@@ -416,6 +420,35 @@ int prepare(span_model* m, int64_t T, int64_t R, const int32_t* h_rows, const in
   return SPAN_OK;
 }
 
+// The head norms of layer l on the q|k|v rows of T compact rows, into q, k, v at their
+// attention rows (of R).
+int norm_heads(span_model* m, int l, int64_t T, int64_t R, hipStream_t s) {
+  const span_model_config& c = m->cfg;
+  const int64_t hq = c.num_q_heads, hkv = c.num_kv_heads, d = c.head_dim;
+  span_qk_norm a{};
+  a.q = m->qkv.p;
+  a.k = m->qkv.as<char>() + hq * d * 2;
+  a.v = m->qkv.as<char>() + (hq + hkv) * d * 2;
+  a.q_out = m->q.p;
+  a.k_out = m->k.p;
+  a.v_out = m->v.p;
+  a.q_gain = m->q_norm.empty() ? nullptr : m->q_norm[l];
+  a.k_gain = m->k_norm.empty() ? nullptr : m->k_norm[l];
+  a.rows = m->rows.as<int32_t>();
+  a.q_stride = a.k_stride = a.v_stride = (hq + 2 * hkv) * d;
+  a.q_out_stride = hq * d;
+  a.k_out_stride = a.v_out_stride = hkv * d;
+  a.n_rows = T;
+  a.out_rows = R;
+  a.num_q_heads = c.num_q_heads;
+  a.num_kv_heads = c.num_kv_heads;
+  a.head_dim = c.head_dim;
+  a.dtype = SPAN_BF16;
+  a.device = m->device;
+  a.eps = c.rms_eps;
+  return span_qk_norm_rope(&a, s);
+}
+
 // Embeddings of the T compact rows, then n_layers decoder layers; attn(l) runs the
 // span attention of layer l on the q/k/v/o buffers.  base >= 0: compact row i is
 // attention row base + i for every i, so the output projection reads the attention
@@ -431,55 +464,30 @@ int run_layers(span_model* m, int64_t T, int n_layers, int64_t base, int64_t R, 
   hipError_t e = launch_copy_rows(m->x.p, c.embed, m->toks.as<int32_t>(), T, H * 2, false, s);
   if (e != hipSuccess) return hip_err(e, w + ": embedding");
   // Up to 8 rows: every GEMM is a GEMV whose second pass also does the step after it
-  // (q/k/v split, SwiGLU, the next RMSNorm), bit for bit the separate kernels' result.
-  // Adapters and head norms come between a GEMV and that step, so they take the GEMMs' way.
+  // (q/k/v split, SwiGLU, the next RMSNorm), bit for bit the separate kernels' result;
+  // not where an adapter or a head norm comes between the two.
   const bool normed_heads = !m->q_norm.empty() || !m->k_norm.empty();
-  const bool gv = ad.n == 0 && !normed_heads && m->gemm.gemv_layer(T, qkv_w, H, F, static_cast<int64_t>(hq) * d);
+  const bool gv = m->gemm.gemv_layer(T, qkv_w, H, F, static_cast<int64_t>(hq) * d);
   float* gp = m->gemm.gemv_part.as<float>();
   const size_t gcap = m->gemm.gemv_part.cap;
   const int Ti = static_cast<int>(T);
-  if (gv && n_layers > 0) {
-    e = launch_rmsnorm(m->x.p, nullptr, m->attn_norm[0], m->n.p, T, H, c.rms_eps, s);
-    if (e != hipSuccess) return hip_err(e, w + ": attention norm");
-  }
   bool normed = false;  // m->n already holds the attention norm of layer l
   for (int l = 0; l < n_layers; ++l) {
-    int rc;
-    if (gv) {
+    int rc = SPAN_OK;
+    if (!normed) {
+      e = launch_rmsnorm(m->x.p, nullptr, m->attn_norm[l], m->n.p, T, H, c.rms_eps, s);
+      if (e != hipSuccess) return hip_err(e, w + ": attention norm");
+    }
+    normed = false;
+    if (gv && !normed_heads && !has_adapter(m, kQkv, l, ad)) {
       e = launch_gemv_qkv(m->n.p, m->w_qkv[l], Ti, H, rows, hq * d, hkv * d, m->q.p, m->k.p, m->v.p, gp, gcap, s);
       if (e != hipSuccess) return hip_err(e, w + ": q/k/v GEMV");
     } else {
-      if (!normed) {
-        e = launch_rmsnorm(m->x.p, nullptr, m->attn_norm[l], m->n.p, T, H, c.rms_eps, s);
-        if (e != hipSuccess) return hip_err(e, w + ": attention norm");
-      }
       rc = m->gemm.run(m->n.p, m->w_qkv[l], m->wt_qkv[l], m->qkv.p, T, qkv_w, H, false, s);
+      if (!rc) rc = add_adapter(m, kQkv, l, ad, m->n.p, m->qkv.p, s);
       if (rc) return rc;
-      rc = add_adapter(m, kQkv, l, ad, m->n.p, m->qkv.p, s);
-      if (rc) return rc;
-      if (normed_heads && T > 0) {
-        span_qk_norm a{};
-        a.q = m->qkv.p;
-        a.k = m->qkv.as<char>() + static_cast<int64_t>(hq) * d * 2;
-        a.v = m->qkv.as<char>() + static_cast<int64_t>(hq + hkv) * d * 2;
-        a.q_out = m->q.p;
-        a.k_out = m->k.p;
-        a.v_out = m->v.p;
-        a.q_gain = m->q_norm.empty() ? nullptr : m->q_norm[l];
-        a.k_gain = m->k_norm.empty() ? nullptr : m->k_norm[l];
-        a.rows = rows;
-        a.q_stride = a.k_stride = a.v_stride = qkv_w;
-        a.q_out_stride = hq * d;
-        a.k_out_stride = a.v_out_stride = hkv * d;
-        a.n_rows = T;
-        a.out_rows = R;
-        a.num_q_heads = hq;
-        a.num_kv_heads = hkv;
-        a.head_dim = d;
-        a.dtype = SPAN_BF16;
-        a.device = m->device;
-        a.eps = c.rms_eps;
-        rc = span_qk_norm_rope(&a, s);
+      if (normed_heads) {
+        rc = norm_heads(m, l, T, R, s);
         if (rc) return rc;
       } else {
         e = launch_scatter_qkv(m->qkv.p, rows, T, hq * d, hkv * d, m->q.p, m->k.p, m->v.p, s);
@@ -495,40 +503,38 @@ int run_layers(span_model* m, int64_t T, int n_layers, int64_t base, int64_t R, 
       e = launch_copy_rows(m->oc.p, m->o.p, rows, T, hq * d * 2, false, s);
       if (e != hipSuccess) return hip_err(e, w + ": attention output gather");
     }
-    if (gv) {
+    if (gv && !has_adapter(m, kO, l, ad)) {
       e = launch_gemv_residual_norm(oc, m->w_o[l], m->x.p, Ti, H, hq * d, m->ffn_norm[l], m->n.p, c.rms_eps, gp, gcap,
                                     s);
       if (e != hipSuccess) return hip_err(e, w + ": output GEMV");
+    } else {
+      rc = m->gemm.run(oc, m->w_o[l], m->wt_o[l], m->x.p, T, H, static_cast<int64_t>(hq) * d, true, s);
+      if (!rc) rc = add_adapter(m, kO, l, ad, oc, m->x.p, s);
+      if (rc) return rc;
+      e = launch_rmsnorm(m->x.p, nullptr, m->ffn_norm[l], m->n.p, T, H, c.rms_eps, s);
+      if (e != hipSuccess) return hip_err(e, w + ": ffn norm");
+    }
+    if (gv && !has_adapter(m, kGateUp, l, ad)) {
       e = launch_gemv_swiglu(m->n.p, m->w_gate_up[l], m->act.p, Ti, F, H, gp, gcap, s);
       if (e != hipSuccess) return hip_err(e, w + ": gate/up GEMV");
-      if (l + 1 < n_layers) {
-        e = launch_gemv_residual_norm(m->act.p, m->w_down[l], m->x.p, Ti, H, F, m->attn_norm[l + 1], m->n.p,
-                                      c.rms_eps, gp, gcap, s);
-        if (e != hipSuccess) return hip_err(e, w + ": down GEMV");
-      } else {
-        rc = m->gemm.run(m->act.p, m->w_down[l], m->wt_down[l], m->x.p, T, H, F, true, s);
-        if (rc) return rc;
-      }
-      continue;
-    }
-    rc = m->gemm.run(oc, m->w_o[l], m->wt_o[l], m->x.p, T, H, static_cast<int64_t>(hq) * d, true, s);
-    if (!rc) rc = add_adapter(m, kO, l, ad, oc, m->x.p, s);
-    if (rc) return rc;
-    e = launch_rmsnorm(m->x.p, nullptr, m->ffn_norm[l], m->n.p, T, H, c.rms_eps, s);
-    if (e != hipSuccess) return hip_err(e, w + ": ffn norm");
-    rc = m->gemm.run(m->n.p, m->w_gate_up[l], m->wt_gate_up[l], m->gu.p, T, 2 * static_cast<int64_t>(F), H, false, s);
-    if (!rc) rc = add_adapter(m, kGateUp, l, ad, m->n.p, m->gu.p, s);
-    if (rc) return rc;
-    e = launch_swiglu(m->gu.p, m->act.p, T, F, s);
-    if (e != hipSuccess) return hip_err(e, w + ": swiglu");
-    const bool adapted_down = ad.n > 0 && !m->adapter_a[kDown].empty() && m->adapter_a[kDown][l];
-    if (l + 1 < n_layers && !adapted_down) {
-      rc = m->gemm.run_norm(m->act.p, m->w_down[l], m->wt_down[l], m->x.p, T, H, F, m->attn_norm[l + 1], m->n.p,
-                            c.rms_eps, &normed, s);
     } else {
+      rc = m->gemm.run(m->n.p, m->w_gate_up[l], m->wt_gate_up[l], m->gu.p, T, 2 * static_cast<int64_t>(F), H, false, s);
+      if (!rc) rc = add_adapter(m, kGateUp, l, ad, m->n.p, m->gu.p, s);
+      if (rc) return rc;
+      e = launch_swiglu(m->gu.p, m->act.p, T, F, s);
+      if (e != hipSuccess) return hip_err(e, w + ": swiglu");
+    }
+    if (l + 1 == n_layers || has_adapter(m, kDown, l, ad)) {
       rc = m->gemm.run(m->act.p, m->w_down[l], m->wt_down[l], m->x.p, T, H, F, true, s);
       if (!rc) rc = add_adapter(m, kDown, l, ad, m->act.p, m->x.p, s);
-      normed = false;
+    } else if (gv) {
+      e = launch_gemv_residual_norm(m->act.p, m->w_down[l], m->x.p, Ti, H, F, m->attn_norm[l + 1], m->n.p, c.rms_eps,
+                                    gp, gcap, s);
+      if (e != hipSuccess) return hip_err(e, w + ": down GEMV");
+      normed = true;
+    } else {
+      rc = m->gemm.run_norm(m->act.p, m->w_down[l], m->wt_down[l], m->x.p, T, H, F, m->attn_norm[l + 1], m->n.p,
+                            c.rms_eps, &normed, s);
     }
     if (rc) return rc;
   }

@@ -7,12 +7,12 @@
 // order, the product with B, scale and base added, rounded once.  Between them, for many
 // rows, the partials are summed once (finish), where few rows' expand does it as it goes.
 //
-// Few rows (a decode step, kFewRows at most): the rows of one adapter, up to 16 at a time,
+// Few rows (a decode step): the rows of one adapter, up to 16 at a time,
 // wherever they lie in the call, are one group, found from the ids by the work-groups
 // themselves, so that each adapter's weights are read once.  Many rows (prefilled
-// segments): tiles of 64 in the caller's order, worked once for each adapter that occurs in
-// one, mostly one.  So nothing is sorted, ids stay on the device and may change between
-// replays of a captured call.
+// segments, large decode steps): a launch of its own orders the rows by adapter, and tiles of
+// 64 ordered rows are worked once for each adapter that occurs in one, mostly one.  The ids
+// stay on the device and may change between replays of a captured call.
 //
 // Matrix instructions 16x16x32, every operand 16 bytes of a row.  The second product's
 // columns are dealt to its tiles so that a lane's results of all tiles are columns that
@@ -37,7 +37,7 @@ using mfma::lo_bf16;
 using mfma::pack_bf16x2;
 
 constexpr int kTile = 16;      // rows of a group, ranks of a block
-constexpr int kFewRows = 256;  // up to here the rows are grouped by adapter
+constexpr int kFewRows = 256;  // at most, of the few-row form (few_rows)
 constexpr int kFewSlices = 8;  // work-groups over K for few rows, whose partials expand adds up
 constexpr int kManySlices = 16;
 constexpr int kManyGroups = 4;
@@ -63,6 +63,7 @@ struct Shape {
   const int32_t* ranks;
   float* part;   // [slices][rows][h_cols] fp32
   bf16_t* h;     // many rows: [rows][h_cols / 16][high 16, low 16]
+  int2* order;   // many rows: {row, its adapter or -1}, each adapter's rows together; H lies in this order
   int64_t rows, x_stride, base_stride, out_stride;
   int K, R, n_adapters, n_parts;
   int N;         // columns of all parts
@@ -145,11 +146,55 @@ __device__ __forceinline__ float4 operator+(const float4& a, const float4& b) {
   return float4{a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w};
 }
 
-// H of one group (few) or of a tile of 64 rows: one slice of K, C::kCols column tiles.
+// Many rows: their order, by adapter, rows without one last (adapters that are equal modulo
+// the number of the others' buckets lie among each other, which costs time, nothing else).  One
+// work-group counts each bucket's rows, adds the counts up and gives every row its place; which
+// of a bucket's rows comes first may change from run to run, and no result depends on it.
+constexpr int kOrderThreads = 1024;  // and buckets
+__global__ __launch_bounds__(kOrderThreads) void adapter_order_kernel(const Shape s) {
+  __shared__ int place[kOrderThreads];
+  __shared__ int sums[kOrderThreads / 64];
+  const int t = threadIdx.x, lane = t & 63, n = static_cast<int>(s.rows);
+  // The next places of a row's bucket: where a wave's rows are all of one, as in a prefilled
+  // segment, one lane takes them all.
+  auto take = [&](int id) {
+    const int bucket = id < 0 ? kOrderThreads - 1 : id % (kOrderThreads - 1);
+    const int first = __builtin_amdgcn_readfirstlane(bucket);
+    const unsigned long long all = __ballot(true);
+    if (__ballot(bucket != first) != 0) return atomicAdd(&place[bucket], 1);
+    const int before = __popcll(all & ((1ull << lane) - 1));
+    int at = 0;
+    if (before == 0) at = atomicAdd(&place[bucket], __popcll(all));
+    return __builtin_amdgcn_readfirstlane(at) + before;
+  };
+  place[t] = 0;
+  __syncthreads();
+  for (int i = t; i < n; i += kOrderThreads) take(adapter_of(s, i));
+  __syncthreads();
+  const int mine = place[t];
+  int upto = mine;  // sum of the wave's buckets up to this one
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int v = __shfl_up(upto, d);
+    upto += lane >= d ? v : 0;
+  }
+  if (lane == 63) sums[wave_id()] = upto;
+  __syncthreads();
+  int before = upto - mine;
+  for (int w = 0; w < wave_id(); ++w) before += sums[w];
+  place[t] = before;
+  __syncthreads();
+  for (int i = t; i < n; i += kOrderThreads) {
+    const int id = adapter_of(s, i);
+    s.order[take(id)] = int2{i, id};
+  }
+}
+
+// H of one group (few) or of a tile of 64 ordered rows: one slice of K, C::kCols column tiles.
 template <bool kFew, class C>
 __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Shape s) {
   __shared__ float4 red[C::kWaves][C::kCols][16 * C::kRows][4];
-  __shared__ int list[kTile];
+  __shared__ int list[16 * C::kRows];  // rows of the call
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int col_groups = (s.h_cols / 16 + C::kCols - 1) / C::kCols;
   const int slice = blockIdx.x / col_groups, ct0 = (blockIdx.x % col_groups) * C::kCols;
@@ -158,8 +203,8 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
   const int k0 = slice * s.k_slice + wave * sub;
   const int k1 = min(s.K, k0 + sub);
   const int m = lane & 15, g = lane >> 4;
-  // row_at(i): row of the call of row i of the group or tile
-  auto work = [&](int aid, unsigned long long mine, auto row_at) {
+  // h_row(i): where H of row i of the group or tile goes
+  auto work = [&](int aid, unsigned long long mine, auto h_row) {
     const int rank = rank_of(s, aid);
     // Rows outside the group and ranks past the adapter's are read as the group's first row and
     // rank: no result of theirs is used, and no load needs a branch.
@@ -167,7 +212,7 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
     const bf16_t* xp[C::kRows];
 #pragma unroll
     for (int t = 0; t < C::kRows; ++t)
-      xp[t] = s.x + row_at((mine >> (16 * t + m)) & 1 ? 16 * t + m : row1) * s.x_stride + 8 * g;
+      xp[t] = s.x + list[(mine >> (16 * t + m)) & 1 ? 16 * t + m : row1] * s.x_stride + 8 * g;
     const bf16_t* ap[C::kCols];
 #pragma unroll
     for (int c = 0; c < C::kCols; ++c) {
@@ -226,7 +271,7 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
       float4 sum = red[0][c][row][q];
 #pragma unroll
       for (int w = 1; w < C::kWaves; ++w) sum = sum + red[w][c][row][q];
-      const int64_t to = row_at(row);
+      const int64_t to = h_row(row);
       const int r = (ct0 + c) % s.rank_blocks * 16 + 4 * q;  // past the rank H is zero
       sum = float4{r < rank ? sum.x : 0.f, r + 1 < rank ? sum.y : 0.f, r + 2 < rank ? sum.z : 0.f, r + 3 < rank ? sum.w : 0.f};
       if (!kFew && s.slices == 1)
@@ -244,10 +289,13 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
     const int64_t row0 = static_cast<int64_t>(blockIdx.y) * (16 * C::kRows);
     const int64_t row = row0 + lane;
     const unsigned long long live = __ballot(row < s.rows);
+    const int2 at = row < s.rows ? s.order[row] : int2{0, -1};
+    if (wave == 0) list[lane] = at.x;
+    __syncthreads();
     // the tile's adapters are dealt to kManyGroups work-groups: where a tile holds the end of one
     // request and the start of the next, neither waits for the other
     int n = 0;
-    for_adapters(adapter_of(s, row), live, [&](int aid, unsigned long long mine) {
+    for_adapters(at.y, live, [&](int aid, unsigned long long mine) {
       if (aid >= 0 && n++ % kManyGroups == static_cast<int>(blockIdx.z))
         work(aid, mine, [&](int i) -> int64_t { return row0 + i; });
     });
@@ -304,21 +352,20 @@ struct Out {
     const uint4 v = *reinterpret_cast<const uint4*>(part + static_cast<uint32_t>(2 * (col * s.R + (r0 < s.R ? r0 : 0))));
     return whole ? v : first_of(v, rank - r0);
   }
-  // Row r of the work-group's (below 2^8; strides are at most 2^23: 32-bit offsets in bytes).
   static __device__ __forceinline__ Vec base(const bf16_t* rows, int64_t stride, const Cols& c, int r, int m) {
-    const int col = c.n0 + J * m < c.width ? c.n0 + J * m : 0;
-    const Vec* p = reinterpret_cast<const Vec*>(reinterpret_cast<const char*>(rows) + offset(r, stride, col));
+    const Vec* p = reinterpret_cast<const Vec*>(rows + offset(r, stride, c.n0 + J * m < c.width ? c.n0 + J * m : 0));
     return kStream ? __builtin_nontemporal_load(p) : *p;
   }
   static __device__ __forceinline__ void store(bf16_t* rows, int64_t stride, const Cols& c, int r, int m, const Vec& v) {
-    Vec* p = reinterpret_cast<Vec*>(reinterpret_cast<char*>(rows) + offset(r, stride, c.n0 + J * m));
+    Vec* p = reinterpret_cast<Vec*>(rows + offset(r, stride, c.n0 + J * m));
     if (kStream)
       __builtin_nontemporal_store(v, p);
     else
       *p = v;
   }
-  static __device__ __forceinline__ uint32_t offset(int r, int64_t stride, int col) {
-    return 2 * (static_cast<uint32_t>(r) * static_cast<uint32_t>(stride) + static_cast<uint32_t>(col));
+  // (strides are at most 2^23: one 32 x 32 bit product)
+  static __device__ __forceinline__ uint64_t offset(int r, int64_t stride, int col) {
+    return static_cast<uint64_t>(static_cast<uint32_t>(r)) * static_cast<uint32_t>(stride) + static_cast<uint32_t>(col);
   }
   // base + scale * row i of the tiles' results
   static __device__ __forceinline__ Vec add(const Vec& base, const f32x4_t (&acc)[J], int i, float scale) {
@@ -434,8 +481,8 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
   using O = Out<J, true>;
   const int lane = threadIdx.x & 63;
   const int m = lane & 15, g = lane >> 4;
+  __shared__ int list[16 * kManyRun];  // rows of the call
   const Cols cols = cols_of<J>(s, blockIdx.x, wave_id());
-  if (cols.n0 >= cols.width) return;
   const bool in_place = s.base == s.out && s.base_stride == s.out_stride;
   const bool has_col = cols.n0 + J * m < cols.width;
   const int64_t row0 = static_cast<int64_t>(blockIdx.y) * (16 * s.run);
@@ -443,9 +490,12 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
   int ids[(16 * kManyRun + 63) / 64];
 #pragma unroll
   for (int i = 0; i < (16 * kManyRun + 63) / 64; ++i) {
-    ids[i] = -1;
-    if (64 * i + lane < n_rows) ids[i] = adapter_of(s, row0 + 64 * i + lane);
+    const int2 at = 64 * i + lane < n_rows ? s.order[row0 + 64 * i + lane] : int2{0, -1};
+    ids[i] = at.y;
+    if (wave_id() == 0 && 64 * i + lane < n_rows) list[64 * i + lane] = at.x;
   }
+  __syncthreads();
+  if (cols.n0 >= cols.width) return;
   const char* h0 = reinterpret_cast<const char*>(s.h + 2 * (row0 * s.h_cols + cols.part * s.rank_blocks * 16));
   // Of H, 16 bytes: ranks 8 (g & 1) .. of block rb, the high (g < 2) or low parts.  Rows past
   // the last are read as the last, other adapters' rows as they are: no result of theirs is used.
@@ -453,8 +503,8 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
     const uint32_t at = 4 * min(r, n_rows - 1) * s.h_cols + 64 * min(rb, s.rank_blocks - 1) + 16 * g;
     return *reinterpret_cast<const uint4*>(h0 + at);
   };
-  const bf16_t* base = s.base + row0 * s.base_stride + cols.col0;
-  bf16_t* out = s.out + row0 * s.out_stride + cols.col0;
+  const bf16_t* base = s.base + cols.col0;
+  bf16_t* out = s.out + cols.col0;
   struct Ahead {
     typename O::Vec base[4];
     uint4 h[kKept];
@@ -463,7 +513,7 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
 #pragma unroll
     for (int k = 0; k < kKept; ++k) a.h[k] = load_h(16 * t + m, k);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a.base[i] = O::base(base, s.base_stride, cols, min(16 * t + 4 * g + i, n_rows - 1), m);
+    for (int i = 0; i < 4; ++i) a.base[i] = O::base(base, s.base_stride, cols, list[min(16 * t + 4 * g + i, n_rows - 1)], m);
   };
   uint4 wv[kKept][J];
   int kept = -1, rank = 0;
@@ -520,7 +570,7 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
       multiply(now, t, acc);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        O::store(out, s.out_stride, cols, 16 * t + 4 * g + i, m, O::add(now.base[i], acc, i, scale));
+        O::store(out, s.out_stride, cols, list[16 * t + 4 * g + i], m, O::add(now.base[i], acc, i, scale));
     }
     return;
   }
@@ -538,7 +588,7 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         if (has_col && ((mine >> (4 * g + i)) & 1))
-          O::store(out, s.out_stride, cols, 16 * t + 4 * g + i, m, aid < 0 ? now.base[i] : O::add(now.base[i], acc, i, scale));
+          O::store(out, s.out_stride, cols, list[16 * t + 4 * g + i], m, aid < 0 ? now.base[i] : O::add(now.base[i], acc, i, scale));
     });
   }
 }
@@ -547,6 +597,13 @@ template <class C>
 unsigned h_groups(const Shape& s) {
   return (s.h_cols / 16 + C::kCols - 1) / C::kCols;
 }
+
+// Rows up to which the few-row form serves.  It reads B again for each 16 rows of an adapter,
+// the many-row form orders the rows first and gains by long runs.  Captured calls of K 4096, few /
+// many in us, 1 adapter and 32 mixed ones:
+//   N 4096, rank 16:   130 rows 15.0 / 14.4, 10.0 / 30.7   256 rows 20.2 / 14.6, 12.8 / 21.1
+//   N 28672, rank 32:   96 rows 25.7 / 19.1, 39.7 / 55.8   192 rows 42.7 / 22.1, 54.1 / 46.5
+int few_rows(const Shape& s) { return s.N <= 8192 ? kFewRows : kFewRows / 2; }
 
 // `rows` rows of the call from `first` on; *bytes: of the workspace they need.
 Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows, size_t* bytes) {
@@ -571,7 +628,7 @@ Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows, size_t* 
   s.rank_blocks = (s.R + 15) / 16;
   s.h_cols = 16 * s.n_parts * s.rank_blocks;
   // K slices: enough work-groups for the chip
-  const bool few = rows <= kFewRows;
+  const bool few = rows <= few_rows(s);
   const int unit = 32 * (few ? FewShrink::kSteps * FewShrink::kWaves : ManyShrink::kSteps * ManyShrink::kWaves);
   const int64_t most = (s.K + unit - 1) / unit;
   const int64_t tiles = (rows + 16 * kManyTiles - 1) / (16 * kManyTiles) * h_groups<ManyShrink>(s);
@@ -584,7 +641,9 @@ Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows, size_t* 
   s.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kManyRun, (rows + 15) / 16 * col_blocks<kManyJ>(s) / 512)));
   s.part = static_cast<float*>(c.workspace);
   s.h = reinterpret_cast<bf16_t*>(s.part + planes * rows * s.h_cols);
-  *bytes = static_cast<size_t>((planes + (few ? 0 : 1)) * rows * s.h_cols) * sizeof(float);
+  s.order = reinterpret_cast<int2*>(s.part + (planes + 1) * rows * s.h_cols);
+  *bytes = few ? planes * rows * s.h_cols * sizeof(float)
+               : (planes + 1) * rows * s.h_cols * sizeof(float) + rows * sizeof(int2);
   return s;
 }
 
@@ -610,7 +669,7 @@ hipError_t launch_adapter_apply(const span_adapter_call& a, hipStream_t st) {
     size_t bytes = 0;
     const Shape s = shape_of(a, first, std::min(kRowsAtOnce, a.n_rows - first), &bytes);
     hipError_t e = hipSuccess;
-    if (s.rows <= kFewRows) {
+    if (s.rows <= few_rows(s)) {
       const unsigned rows = static_cast<unsigned>(s.rows);
       adapter_shrink_kernel<true, FewShrink><<<dim3(s.slices * h_groups<FewShrink>(s), rows), 64 * FewShrink::kWaves, 0, st>>>(s);
       e = hipGetLastError();
@@ -618,6 +677,9 @@ hipError_t launch_adapter_apply(const span_adapter_call& a, hipStream_t st) {
       adapter_expand_few_kernel<<<dim3(col_blocks<kFewJ>(s), rows), 64 * kExpandWaves, 0, st>>>(s);
     } else {
       const unsigned tiles = static_cast<unsigned>((s.rows + 16 * kManyTiles - 1) / (16 * kManyTiles));
+      adapter_order_kernel<<<1, kOrderThreads, 0, st>>>(s);
+      e = hipGetLastError();
+      if (e != hipSuccess) return e;
       adapter_shrink_kernel<false, ManyShrink><<<dim3(s.slices * h_groups<ManyShrink>(s), tiles, kManyGroups), 64 * ManyShrink::kWaves, 0, st>>>(s);
       e = hipGetLastError();
       if (e == hipSuccess && s.slices > 1) {

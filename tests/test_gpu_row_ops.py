@@ -289,6 +289,32 @@ def test_adapters_in_a_graph_follow_their_ids_and_share_no_workspace():
             assert torch.equal(want, outs[i]), (step, i)
 
 
+@pytest.mark.parametrize("T,S", [(300, 6), (700, 2100), (129, 40), (70000, 9)])
+def test_adapters_of_many_mixed_rows_in_a_graph(T, S):
+    """Rows ordered by adapter on the device: more adapters than a work-group counts apart, more
+    rows than are worked at once, ids that change between replays, runs of one adapter."""
+    parts = (8, 8200) if T == 129 else (8,)
+    case = _adapt_case(T, 16, parts, 8, S, seed=T)
+    print(f"mixed adapters T {T} S {S}", flush=True)
+    d = [t.cuda() for t in case]
+    out, want = torch.empty_like(d[1]), torch.empty_like(d[1])
+    ids = d[2].clone()
+    ws = torch.empty(spanq.adapter_workspace(T, 16, 8, parts), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        spanq.adapter_apply(d[0], d[1], ids, d[3], d[4], d[5], out, parts=parts, ranks=d[6], workspace=ws)
+    at = torch.arange(T)
+    for i, new in enumerate((case[2], case[2].sort().values, torch.full((T,), S - 1), at // 65 % S, at * 1023 % S - 1)):
+        ids.copy_(new.to(torch.int32))
+        out.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        _check_adapt(out.cpu(), (case[0], case[1], new.to(torch.int32)) + case[3:], parts, f"ids {i}")
+        spanq.adapter_apply(d[0], d[1], ids, d[3], d[4], d[5], want, parts=parts, ranks=d[6])
+        assert torch.equal(want, out)
+
+
 def test_row_operators_on_another_stream():
     """Work on a stream of its own, workspace taken there, ordered by an event alone."""
     side = torch.cuda.Stream()

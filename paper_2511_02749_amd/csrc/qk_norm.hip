@@ -9,9 +9,8 @@
 //
 // A lane holds 16 bytes of the head's first half and the 16 bytes d/2 further on, so both
 // members of a pair are in one lane, the sum of squares takes log2(lanes per head) lane
-// exchanges, and every access is a 16-byte vector.  A work-group takes kRows rows: it puts
-// their cos and sin into LDS once (all heads of a row share them), then walks the rows'
-// heads.  Angles are formed in 64 bits, in turns, and reduced to half a turn before the
+// exchanges, and every access is a 16-byte vector.  A work-group takes one row: it puts its
+// cos and sin into LDS once (all heads share them), then walks the heads.  Angles are formed in 64 bits, in turns, and reduced to half a turn before the
 // 32-bit sine: at position 120000 a 32-bit product would be off by 0.004 radians.  Sums,
 // norm and rotation are 32-bit; the only rounding to 16 bits is the result's.
 #include <hip/hip_runtime.h>
@@ -19,6 +18,7 @@
 #include <cmath>
 
 #include "dev_common.h"
+#include "grid.h"
 #include "page_write.h"
 #include "row_ops.h"
 
@@ -30,40 +30,36 @@ constexpr int kThreads = 256;
 struct QkArgs {
   span_qk_norm a;
   double log2_theta;
+  int64_t row0;  // first row of the launch
 };
 
-template <typename T, int D, int kRows>
+template <typename T, int D>
 __global__ __launch_bounds__(kThreads) void qk_norm_kernel(const QkArgs g) {
   constexpr int E = Chunk16<T>::E;
   constexpr int H = D / 2;
   constexpr int L = H / E;  // lanes per head
   constexpr int G = kThreads / L;
-  __shared__ float2 turn[kRows][H];
+  __shared__ float2 turn[H];
   const span_qk_norm& a = g.a;
-  const int64_t r0 = static_cast<int64_t>(blockIdx.x) * kRows;
+  const int64_t row = g.row0 + blockIdx.x;
+  const int64_t to = a.rows ? a.rows[row] : row;
+  if (to < 0 || to >= a.out_rows) return;
   if (a.positions) {
-    for (int e = threadIdx.x; e < kRows * H; e += kThreads) {
-      const int i = e % H;
-      if (r0 + e / H >= a.n_rows) break;
+    if (const int i = threadIdx.x; i < H) {
       const double inv = exp2(-2.0 * i / D * g.log2_theta) * 0.15915494309189533577;  // turns per position
-      double t = static_cast<double>(a.positions[r0 + e / H]) * inv;
+      double t = static_cast<double>(a.positions[row]) * inv;
       t -= rint(t);
       float sn, cs;
       sincospif(static_cast<float>(2.0 * t), &sn, &cs);
-      turn[e / H][i] = float2{cs, sn};
+      turn[i] = float2{cs, sn};
     }
     __syncthreads();
   }
   const int nq = a.q ? a.num_q_heads : 0, nk = a.k ? a.num_kv_heads : 0, nv = a.v ? a.num_kv_heads : 0;
   const int heads = nq + nk + nv;
   const int c = threadIdx.x % L;
-  for (int e = threadIdx.x / L; e < kRows * heads; e += G) {
-    const int j = e / heads;
-    int h = e - j * heads;
-    const int64_t row = r0 + j;
-    if (row >= a.n_rows) break;
-    const int64_t to = a.rows ? a.rows[row] : row;
-    if (to < 0 || to >= a.out_rows) continue;
+  for (int e = threadIdx.x / L; e < heads; e += G) {
+    int h = e;
     const T* src;
     T* dst;
     const T* gain = nullptr;
@@ -111,7 +107,7 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(const QkArgs g) {
       if (rotate) {
 #pragma unroll
         for (int u = 0; u < E; ++u) {
-          const float2 t = turn[j][c * E + u];
+          const float2 t = turn[c * E + u];
           const float lo = y0[u] * t.x - y1[u] * t.y;
           y1[u] = y1[u] * t.x + y0[u] * t.y;
           y0[u] = lo;
@@ -130,9 +126,12 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(const QkArgs g) {
 
 template <typename T, int D>
 hipError_t launch_d(const span_qk_norm& a, hipStream_t s) {
-  QkArgs g{a, std::log2(static_cast<double>(a.rope_theta))};
-  qk_norm_kernel<T, D, 1><<<static_cast<unsigned>(a.n_rows), kThreads, 0, s>>>(g);
-  return hipGetLastError();
+  QkArgs g{a, std::log2(static_cast<double>(a.rope_theta)), 0};
+  return launch_in_slices(a.n_rows, kThreads, hipErrorInvalidValue, [&](int64_t first, int64_t count) {
+    g.row0 = first;
+    qk_norm_kernel<T, D><<<static_cast<unsigned>(count), kThreads, 0, s>>>(g);
+    return hipGetLastError();
+  });
 }
 
 }  // namespace

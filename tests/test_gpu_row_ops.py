@@ -132,6 +132,17 @@ def test_head_norms_of_zero_and_nonfinite_heads():
     assert float((y.double() - ref)[fine].abs().max()) < 1e-5
 
 
+def test_head_norms_of_more_rows_than_a_grid_takes():
+    n, d = (1 << 24) + 3, 64
+    x = torch.randn(n, 1, d, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda", dtype=torch.bfloat16)
+    gain = torch.ones(d, dtype=torch.bfloat16, device="cuda")
+    y = torch.zeros_like(x)
+    spanq.qk_norm_rope(x, None, None, gain, None, 1e-5, y, None, None)
+    for rows in (slice(0, 100), slice((1 << 24) - 50, n)):  # both ends of the first launch, and the second
+        _check_heads(y[rows].cpu(), x[rows].cpu(), gain.cpu(), 1e-5, None, 1e4, str(rows))
+    assert bool((y != 0).any(-1).all())
+
+
 # ------------------------------------------------------------------------ adapters
 
 def _adapt_exact(x, base, ids, a, b, scale, ranks, parts):

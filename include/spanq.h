@@ -582,7 +582,8 @@ int span_qk_norm_rope(const span_qk_norm* args, void* stream);
  * column parts (q|k|v, gate|up) has an A for each part and a B over all columns.  Rows
  * come in any order; rows whose id lies outside [0, n_adapters) get base[i].
  * In place: out == base with the same stride.  A row's result depends on its own x, base
- * and adapter, and in its last bits on the number of rows of the call. */
+ * and adapter, and in its last bits on the sizes of the call (of more than 65536 rows: on its
+ * place in it too). */
 typedef struct {
   const void* x;      /* [n_rows][in_features] */
   const void* base;   /* [n_rows][out], out = the sum of part_cols: the projection's result */
@@ -606,7 +607,7 @@ typedef struct {
   int32_t device;
   int32_t reserved;   /* 0 */
 } span_adapter_call;
-/* Workspace of a call: from n_rows, in_features, max_rank and n_parts. */
+/* Workspace of a call: from n_rows, in_features, max_rank, n_parts and part_cols. */
 int span_adapter_workspace(const span_adapter_call* args, size_t* bytes);
 int span_adapter_apply(const span_adapter_call* args, void* stream);
 

@@ -649,8 +649,8 @@ Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows, size_t* 
 
 }  // namespace
 
-// Rows worked at once: grids stay below 2^32 threads (at most 2^20 / 512 + 4 work-groups of 256
-// threads across, a 32nd of the rows down).
+// Rows worked at once: grids stay below 2^32 threads (expand: at most 2^20 / 256 + 4 work-groups of
+// 256 threads across, and down 2^16 / 128, as runs are whole where there are that many).
 constexpr int64_t kRowsAtOnce = int64_t{1} << 16;
 
 size_t adapter_workspace_bytes(const span_adapter_call& a) {

@@ -40,12 +40,15 @@ class CallStats:
 def lookup_drafts(tokens: Sequence[int], n: int, longest: int = 3) -> List[int]:
     """Up to n tokens that followed the latest earlier place of the last tokens: of the last
     `longest`, else of fewer, down to one; [] if even that stands nowhere else."""
-    toks = list(tokens)
+    toks = np.asarray(tokens, np.int32)
     for m in range(min(longest, len(toks) - 1), 0, -1):
-        tail = toks[-m:]
-        for at in range(len(toks) - m - 1, -1, -1):
-            if toks[at:at + m] == tail:
-                return toks[at + m:at + m + n]
+        starts = len(toks) - m  # of earlier places
+        same = toks[:starts] == toks[starts]
+        for i in range(1, m):
+            same &= toks[i:starts + i] == toks[starts + i]
+        at = np.flatnonzero(same)
+        if at.size:
+            return toks[at[-1] + m:at[-1] + m + n].tolist()
     return []
 
 
@@ -124,10 +127,16 @@ class Engine:
     def _decode_checked(self, plan, history, out, max_tokens: int):
         """Steps of drafts and sampled tokens until every query has max_tokens; (drafts fed, kept)."""
         n, fed, kept = len(out), 0, 0
+        seen = []  # each query's own tokens, with room for those to come
+        for h, o in zip(history, out):
+            seen.append(np.empty(len(h) + max_tokens, np.int32))
+            seen[-1][:len(h) + len(o)] = h + o
         while any(len(o) < max_tokens for o in out):
             open_ = [len(o) < max_tokens for o in out]
-            drafts = [lookup_drafts(h + o, min(self.n_drafts, max_tokens - len(o) - 1)) if go else []
-                      for h, o, go in zip(history, out, open_)]
+            if any(o[-1] < 0 for o in out):
+                raise RuntimeError("a query's logits leave no token any weight")
+            drafts = [lookup_drafts(s[:len(h) + len(o)], min(self.n_drafts, max_tokens - len(o) - 1)) if go else []
+                      for s, h, o, go in zip(seen, history, out, open_)]
             got = self.model.decode_drafts(
                 plan, [o[-1] if go else -1 for o, go in zip(out, open_)], drafts,
                 u_accept=[self._rng.random(len(d), np.float32) for d in drafts],
@@ -135,7 +144,8 @@ class Engine:
                 stream=self.stream)
             fed += sum(len(d) for d in drafts)
             kept += sum(len(g) - 1 for g in got if g)
-            for o, g in zip(out, got):
+            for s, h, o, g in zip(seen, history, out, got):
+                s[len(h) + len(o):len(h) + len(o) + len(g)] = g
                 o.extend(g)
         return fed, kept
 

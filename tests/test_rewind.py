@@ -122,6 +122,44 @@ def test_lookup_drafts():
     assert lookup_drafts([1, 2, 3, 9, 7, 3], 5) == [9, 7, 3]
     assert lookup_drafts([1, 2, 3], 4) == [] and lookup_drafts([], 4) == [] and lookup_drafts([5, 5], 0) == []
     assert lookup_drafts([5, 5, 5, 5], 3) == [5]
+    rng = np.random.default_rng(0)
+    for n in range(60):
+        toks = rng.integers(0, 3, n).tolist()
+        want = []
+        for m in (3, 2, 1):  # as it is said: the latest earlier place of the last m, the longest m first
+            at = [i for i in range(n - m) if toks[i:i + m] == toks[n - m:]] if m < n else []
+            if at:
+                want = toks[at[-1] + m:at[-1] + m + 4]
+                break
+        assert lookup_drafts(toks, 4) == want == lookup_drafts(np.array(toks, np.int32), 4)
+
+
+class _NoWeight:
+    """A pool, its plan and its model in one, whose second step finds no token with any weight."""
+
+    def plan(self, queries, stream):
+        self.steps = 0
+        return self
+
+    def forward(self, plan, rows, stream=None):
+        return [7]
+
+    def decode_drafts(self, plan, tokens, drafts, **_):
+        self.steps += 1
+        assert self.steps < 4
+        return [[-1] if t >= 0 else [] for t in tokens]
+
+    def destroy(self):
+        self.steps = None
+
+
+def test_engine_ends_where_no_token_has_any_weight():
+    from paper_2511_02749_amd import spanquery as sq
+    from paper_2511_02749_amd.engine import Engine
+    fake = _NoWeight()
+    with pytest.raises(RuntimeError, match="weight"):
+        Engine(fake, fake, n_drafts=2).generate_many([sq.Spans(prefix=[], fragments=[], cross=[1, 2])], 5)
+    assert fake.steps is None
 
 
 def _cut(q, c0):

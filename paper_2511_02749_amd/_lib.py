@@ -208,13 +208,22 @@ def _f32p(a: np.ndarray):
     return a.ctypes.data_as(ctypes.POINTER(ctypes.c_float))
 
 
-def _table(seq, layers: int):
-    """A host table of `layers` device pointers (None: a null table)."""
+def _weight(what: str, x, dtype: str, numel: int, device: int) -> Optional[int]:
+    """Device pointer of a weight: a dense tensor of `numel` elements on that GPU, or an address, or None."""
+    if x is not None and not isinstance(x, int) and (
+            x.get_device() != device or str(x.dtype) != f"torch.{dtype}" or x.numel() != numel or not x.is_contiguous()):
+        raise SpanError(SPAN_EINVAL, f"{what} must be contiguous, {dtype}, on GPU {device}, with {numel} elements, not "
+                                     f"{x.dtype} {tuple(x.shape)} on {x.device}")
+    return _ptr(x)
+
+
+def _table(what: str, seq, layers: int, numel: int, device: int):
+    """A host table of `layers` device pointers to bf16 weights (None: a null table)."""
     if seq is None:
         return None
     if len(seq) != layers:
-        raise SpanError(SPAN_EINVAL, "a table needs an entry for each layer")
-    return (ctypes.c_void_p * layers)(*[_ptr(x) for x in seq])
+        raise SpanError(SPAN_EINVAL, f"{what} needs an entry for each layer")
+    return (ctypes.c_void_p * layers)(*[_weight(what, x, "bfloat16", numel, device) for x in seq])
 
 
 def _ptr(x) -> Optional[int]:
@@ -575,8 +584,9 @@ class Model:
     def set_qk_norm(self, q_norm=None, k_norm=None):
         """Head norms of the layers' queries and keys (span_model_set_qk_norm): a gain [head_dim] for
         each layer (None: not normed), or None for none."""
-        L = self.cfg.num_layers
-        _check(load().span_model_set_qk_norm(self._h, _table(q_norm, L), _table(k_norm, L)))
+        L, d, device = self.cfg.num_layers, self.cfg.head_dim, self.pool.cfg.device
+        _check(load().span_model_set_qk_norm(self._h, _table("q_norm", q_norm, L, d, device),
+                                             _table("k_norm", k_norm, L, d, device)))
         self._keep_norms = (q_norm, k_norm)
 
     def set_adapters(self, n_adapters: int = 0, max_rank: int = 0, scale=None, ranks=None, qkv=None, o=None,
@@ -584,11 +594,16 @@ class Model:
         """Low-rank adapters of the projections (span_model_set_adapters): each of qkv, o, gate_up,
         down is None or a pair (a, b) of per-layer sequences of device tensors (an entry may be None),
         a [n, parts, rank, in] and b [n, out, rank].  Without arguments: none."""
-        L = self.cfg.num_layers
-        cfg = ModelAdapters(n_adapters=n_adapters, max_rank=max_rank, scale=_ptr(scale), ranks=_ptr(ranks))
-        for name, pair in (("qkv", qkv), ("o", o), ("gate_up", gate_up), ("down", down)):
-            for side, seq in zip("ab", pair or (None, None)):
-                t = _table(seq, L)
+        c, device = self.cfg, self.pool.cfg.device
+        heads = c.num_q_heads * c.head_dim
+        cfg = ModelAdapters(n_adapters=n_adapters, max_rank=max_rank,
+                            scale=_weight("scale", scale, "float32", n_adapters, device),
+                            ranks=_weight("ranks", ranks, "int32", n_adapters, device))
+        for name, pair, parts, wide, cols in (
+                ("qkv", qkv, 3, c.hidden, heads + 2 * c.num_kv_heads * c.head_dim), ("o", o, 1, heads, c.hidden),
+                ("gate_up", gate_up, 2, c.hidden, 2 * c.ffn), ("down", down, 1, c.ffn, c.hidden)):
+            for side, seq, n in zip("ab", pair or (None, None), (parts * wide, cols)):
+                t = _table(f"{side}_{name}", seq, c.num_layers, n_adapters * max_rank * n, device)
                 if t is not None:
                     setattr(cfg, f"{side}_{name}", ctypes.cast(t, ctypes.POINTER(ctypes.c_void_p)))
         _check(load().span_model_set_adapters(self._h, ctypes.byref(cfg)))
@@ -627,11 +642,11 @@ class Model:
                     if u_accept is not None:
                         ua[q, :nd[q]] = row[:nd[q]]
             rows = int(sum(nd[q] for q in range(n) if t[q] >= 0))
-            if draft_logits is not None and (tuple(draft_logits.shape) != (rows, self.cfg.vocab) or
-                                             not draft_logits.is_contiguous() or draft_logits.dtype != torch.float32):
-                raise SpanError(SPAN_EINVAL, "decode_drafts: draft_logits must be float32 [drafts, vocab]")
+            if draft_logits is not None and tuple(draft_logits.shape) != (rows, self.cfg.vocab):
+                raise SpanError(SPAN_EINVAL, "decode_drafts: draft_logits must be [drafts, vocab]")
             sampling = ctypes.byref(Sampling(u_accept=_f32p(ua), u_sample=_f32p(us), temperature=_f32p(heat),
-                                             draft_logits=_ptr(draft_logits)))
+                                             draft_logits=_weight("draft_logits", draft_logits, "float32",
+                                                                  rows * self.cfg.vocab, self.pool.cfg.device)))
         out, n_out = np.zeros((max(1, n), k + 1), np.int32), np.zeros(max(1, n), np.int32)
         lp = np.zeros((max(1, n), k + 1), np.float32)
         _check(load().span_model_decode_drafts(self._h, plan._h, _i32p(t), _i32p(d) if k else None,

@@ -288,6 +288,32 @@ def test_sampled_steps_follow_their_random_numbers():
     run.close()
 
 
+def test_weights_of_other_sizes_types_and_devices_are_refused():
+    swl = W.stack_small()
+    run = StackRun(swl)
+    sw, bf = swl.weights, torch.bfloat16
+    L, H, F = sw.n_layers, sw.hidden, sw.ffn
+    a, b = torch.zeros(2, 1, 8, F, dtype=bf, device="cuda"), torch.zeros(2, H, 8, dtype=bf, device="cuda")
+    run.model.set_adapters(2, 8, down=([a] * L, [b] * L))
+    for bad in (dict(max_rank=16), dict(down=([a] * L, [b[:1]] * L)), dict(down=([a.cpu()] * L, [b] * L)),
+                dict(down=([a.float()] * L, [b] * L)), dict(down=([a] * (L - 1), [b] * L)), dict(down=([a] * L, None)),
+                dict(scale=torch.ones(2)), dict(scale=torch.ones(1, device="cuda")), dict(ranks=torch.ones(2, device="cuda")),
+                dict(down=([a.transpose(2, 3)] * L, [b] * L))):
+        with pytest.raises(spanq.SpanError) as e:
+            run.model.set_adapters(**{**dict(n_adapters=2, max_rank=8, down=([a] * L, [b] * L)), **bad})
+        assert e.value.code == -1
+    gain = torch.ones(sw.head_dim, dtype=bf, device="cuda")
+    for bad in ([gain] * (L + 1), [gain.float()] * L, [gain[:-8]] * L, [gain.cpu()] * L):
+        with pytest.raises(spanq.SpanError):
+            run.model.set_qk_norm(bad)
+    plan = run.pool.plan(swl.batches[0])
+    toks = run.model.forward(plan, swl.row_tokens)
+    with pytest.raises(spanq.SpanError):  # on the host
+        run.model.decode_drafts(plan, toks, [[1]] * len(toks), draft_logits=torch.zeros(len(toks), sw.vocab))
+    plan.destroy()
+    run.close()
+
+
 @pytest.mark.parametrize("temperature", [0.0, 0.8])
 def test_engine_with_lookup_drafts_and_adapters(temperature):
     """The engine's steps with drafts looked up in each query's own tokens: as many tokens as asked

@@ -607,7 +607,8 @@ typedef struct {
   int32_t device;
   int32_t reserved;   /* 0 */
 } span_adapter_call;
-/* Workspace of a call: from n_rows, in_features, max_rank, n_parts and part_cols. */
+/* Workspace of a call, and of every call that is alike but of fewer rows: from n_rows,
+ * in_features, max_rank, n_parts and part_cols. */
 int span_adapter_workspace(const span_adapter_call* args, size_t* bytes);
 int span_adapter_apply(const span_adapter_call* args, void* stream);
 
@@ -648,7 +649,8 @@ typedef struct {
   int32_t vocab;              /* 1 .. 2^24 */
   int32_t device;
 } span_verify_call;
-/* Workspace of a call: from n_requests, max_drafts and vocab. */
+/* Workspace of a call, and of every call that is alike but of fewer requests: from n_requests,
+ * max_drafts and vocab. */
 int span_verify_workspace(const span_verify_call* args, size_t* bytes);
 int span_verify_drafts(const span_verify_call* args, void* stream);
 

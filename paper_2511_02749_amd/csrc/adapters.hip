@@ -664,6 +664,19 @@ size_t adapter_workspace_bytes(const span_adapter_call& a) {
   return most;
 }
 
+size_t adapter_workspace_up_to(const span_adapter_call& a) {
+  // the most rows of either form, and of each number of K slices, which falls with the tiles
+  size_t most = adapter_workspace_bytes(a), bytes = 0;
+  const auto of = [&](int64_t n) {
+    (void)shape_of(a, 0, n, &bytes);
+    most = std::max(most, bytes);
+  };
+  const int64_t n = std::min(a.n_rows, kRowsAtOnce);
+  for (const int64_t few : {kFewRows / 2, kFewRows}) of(std::min<int64_t>(n, few));
+  for (int64_t rows = 16 * kManyTiles; rows < n && rows <= 256 * 16 * kManyTiles; rows += 16 * kManyTiles) of(rows);
+  return most;
+}
+
 hipError_t launch_adapter_apply(const span_adapter_call& a, hipStream_t st) {
   for (int64_t first = 0; first < a.n_rows; first += kRowsAtOnce) {
     size_t bytes = 0;

@@ -100,7 +100,7 @@ int span_adapter_workspace(const span_adapter_call* args, size_t* bytes) {
   const char* who = "span_adapter_workspace";
   if (!args || !bytes) return bad(who, "null argument");
   if (const char* what = check_adapter_sizes(*args)) return bad(who, what);
-  *bytes = adapter_workspace_bytes(*args);
+  *bytes = adapter_workspace_up_to(*args);
   return SPAN_OK;
 }
 
@@ -133,7 +133,7 @@ int span_verify_workspace(const span_verify_call* args, size_t* bytes) {
   const char* who = "span_verify_workspace";
   if (!args || !bytes) return bad(who, "null argument");
   if (const char* what = check_verify_sizes(*args)) return bad(who, what);
-  *bytes = verify_workspace_bytes(args->n_requests, args->max_drafts, args->vocab);
+  *bytes = verify_workspace_up_to(args->n_requests, args->max_drafts, args->vocab);
   return SPAN_OK;
 }
 

@@ -8,7 +8,7 @@
 //   T <= 0: a draft is kept if it is the argmax of x_j, the next token is the argmax of x_a
 //
 // Three launches (two where no draft has a distribution):
-// 1. every row in chunks of kChunk logits, one wave each: the chunk's largest logit, its
+// 1. every row in chunks of kChunk logits (chunk_of), one wave each: the chunk's largest logit, its
 //    lowest id, and the sum of exp against it;
 // 2. (draft logits) the chunks of the one row that decides a request: sums of max(p - q, 0);
 // 3. one work-group per request: the chunk where the running sum passes u, then the token in
@@ -26,6 +26,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "grid.h"
 #include "row_ops.h"
@@ -35,8 +36,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kChunk = 2048;        // logits of a wave in 1 and 2: 63 chunks of 128256, one for each lane in 3
-constexpr int kPer = kChunk / 64;
 constexpr int kPickThreads = 1024;  // a wave for each row of up to seven drafts and their distributions
 constexpr int kMaxDrafts = SPAN_MAX_DRAFTS;
 constexpr double kLog2e = 1.4426950408889634074;
@@ -171,9 +170,10 @@ __device__ __forceinline__ Request request_of(const span_verify_call& c, int q) 
 typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 __device__ __forceinline__ int id_of(int base, int lane, int u) { return base + 4 * (64 * (u / 4) + lane) + u % 4; }
 
+template <int kPer>
 __device__ __forceinline__ void load_chunk(const float* __restrict__ row, int base, int lane, int vocab,
                                            float (&x)[kPer]) {
-  if (base + kChunk <= vocab) {
+  if (base + 64 * kPer <= vocab) {
 #pragma unroll
     for (int u = 0; u < kPer; u += 4) {
       const f32x4_any v = *reinterpret_cast<const f32x4_any*>(row + id_of(base, lane, u));
@@ -190,7 +190,9 @@ __device__ __forceinline__ void load_chunk(const float* __restrict__ row, int ba
 }
 
 // ------------------------------------------------------------------ 1: chunks of every row
+template <int kChunk>
 __global__ __launch_bounds__(kThreads) void verify_stats_kernel(const Args a) {
+  constexpr int kPer = kChunk / 64;
   const span_verify_call& c = a.c;
   const int q = a.q0 + static_cast<int>(blockIdx.z);
   const int k = c.max_drafts;
@@ -354,7 +356,9 @@ __device__ __forceinline__ Left left_of(const Args& a, int q, const Request& r, 
 }
 
 // ------------------------------------------------------------------ 2: what the deciding row leaves
+template <int kChunk>
 __global__ __launch_bounds__(kThreads) void verify_left_kernel(const Args a) {
+  constexpr int kPer = kChunk / 64;
   __shared__ Verdict v;
   const span_verify_call& c = a.c;
   const int q = a.q0 + static_cast<int>(blockIdx.y);
@@ -377,9 +381,10 @@ __global__ __launch_bounds__(kThreads) void verify_left_kernel(const Args a) {
 }
 
 // ------------------------------------------------------------------ 3: the token
+template <int kChunk>
 __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a) {
   constexpr int kPickWaves = kPickThreads / 64;
-  constexpr int kEach = kChunk / kPickThreads;
+  constexpr int kEach = (kChunk + kPickThreads - 1) / kPickThreads;  // of the first threads, if there are too many
   __shared__ Verdict v;
   __shared__ double s_chunk[kMaxDrafts + 1][64];
   __shared__ double s_wave[kPickWaves];
@@ -457,7 +462,7 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
     }
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
-      w[e] = i0 + e < c.vocab ? l.of(i0 + e, x[e], y[e]) : 0.0;
+      w[e] = i0 + e < min(c.vocab, (chunk + 1) * kChunk) ? l.of(i0 + e, x[e], y[e]) : 0.0;
       mine += w[e];
     }
     const double upto = wave_scan(mine);
@@ -501,19 +506,54 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
   if (threadIdx.x == 0) c.accepted[q] = n;
 }
 
-int chunks_of(int vocab) { return (vocab + kChunk - 1) / kChunk; }
+int64_t chunks_of(int vocab, int chunk) { return (vocab + chunk - 1) / chunk; }
+
+// Logits of a chunk: the fewest of 512, 1024 and 2048 that leave a row at most 64 chunks, one for
+// each lane that adds them up, and all rows at most 2^16.  Small chunks spread few logits over the chip,
+// and are more to add up in 2 and 3.  Four drafts with a distribution, captured calls of 512 / 1024 / 2048 in us:
+//   vocabulary 8000:    8 requests 15.8 / 18.6 / 22.6   64: 22.2 / 24.4 / 27.9   256: 36.5 / 36.2 / 39.5
+//   vocabulary 32768:   8 requests 17.1 / 19.0 / 23.0   64: 34.4 / 34.2 / 35.1   256: 107 / 94 / 89
+bool chunk_fits(int64_t requests, int max_drafts, int vocab, int chunk) {
+  const int64_t n = chunks_of(vocab, chunk);
+  return n <= 64 && requests * (2 * max_drafts + 1) * n <= 1 << 16;
+}
+int chunk_of(int64_t requests, int max_drafts, int vocab) {
+  for (const int chunk : {512, 1024})
+    if (chunk_fits(requests, max_drafts, vocab, chunk)) return chunk;
+  return 2048;
+}
+
+// f(a chunk size as a type)
+template <class F>
+hipError_t with_chunk(int chunk, F f) {
+  switch (chunk) {
+    case 512: return f(std::integral_constant<int, 512>{});
+    case 1024: return f(std::integral_constant<int, 1024>{});
+    default: return f(std::integral_constant<int, 2048>{});
+  }
+}
 
 }  // namespace
 
 size_t verify_workspace_bytes(int64_t n, int max_drafts, int vocab) {
-  const size_t ch = static_cast<size_t>(chunks_of(vocab)), nz = static_cast<size_t>(n), k = max_drafts;
-  return nz * ch * ((2 * k + 1) * sizeof(Stat) + sizeof(double));
+  const int64_t ch = chunks_of(vocab, chunk_of(n, max_drafts, vocab));
+  return static_cast<size_t>(n * ch) * ((2 * static_cast<size_t>(max_drafts) + 1) * sizeof(Stat) + sizeof(double));
+}
+
+size_t verify_workspace_up_to(int64_t n, int max_drafts, int vocab) {
+  size_t most = verify_workspace_bytes(n, max_drafts, vocab);
+  for (const int chunk : {512, 1024}) {  // the most requests that take chunks so small
+    const int64_t ch = chunks_of(vocab, chunk);
+    if (ch <= 64) most = std::max(most, verify_workspace_bytes(std::min(n, (1 << 16) / (ch * (2 * max_drafts + 1))), max_drafts, vocab));
+  }
+  return most;
 }
 
 hipError_t launch_verify_drafts(const span_verify_call& c, hipStream_t s) {
   Args a{};
   a.c = c;
-  a.chunks = chunks_of(c.vocab);
+  const int chunk = chunk_of(c.n_requests, c.max_drafts, c.vocab);
+  a.chunks = static_cast<int>(chunks_of(c.vocab, chunk));
   const size_t n = static_cast<size_t>(c.n_requests), ch = static_cast<size_t>(a.chunks), k = c.max_drafts;
   a.target = static_cast<Stat*>(c.workspace);
   a.draft = a.target + n * (k + 1) * ch;
@@ -525,15 +565,18 @@ hipError_t launch_verify_drafts(const span_verify_call& c, hipStream_t s) {
     a.q0 = static_cast<int>(first);
     const unsigned nq = static_cast<unsigned>(count);
     const unsigned groups = static_cast<unsigned>((a.chunks + kWaves - 1) / kWaves);
-    verify_stats_kernel<<<dim3(groups, rows, nq), kThreads, 0, s>>>(a);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && c.draft_logits && c.max_drafts > 0) {
-      verify_left_kernel<<<dim3(groups, nq), kThreads, 0, s>>>(a);
-      e = hipGetLastError();
-    }
-    if (e != hipSuccess) return e;
-    verify_pick_kernel<<<nq, kPickThreads, 0, s>>>(a);
-    return hipGetLastError();
+    return with_chunk(chunk, [&](auto size) -> hipError_t {
+      constexpr int kChunk = decltype(size)::value;
+      verify_stats_kernel<kChunk><<<dim3(groups, rows, nq), kThreads, 0, s>>>(a);
+      hipError_t e = hipGetLastError();
+      if (e == hipSuccess && c.draft_logits && c.max_drafts > 0) {
+        verify_left_kernel<kChunk><<<dim3(groups, nq), kThreads, 0, s>>>(a);
+        e = hipGetLastError();
+      }
+      if (e != hipSuccess) return e;
+      verify_pick_kernel<kChunk><<<nq, kPickThreads, 0, s>>>(a);
+      return hipGetLastError();
+    });
   });
 }
 

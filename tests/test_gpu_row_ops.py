@@ -326,6 +326,25 @@ def test_adapters_of_many_mixed_rows_in_a_graph(T, S):
         assert torch.equal(want, out)
 
 
+def test_a_workspace_serves_smaller_calls():
+    parts, S, R, K, V = (520,), 5, 24, 512, 5000
+    ws = torch.empty(spanq.adapter_workspace(900, K, R, parts), dtype=torch.uint8, device="cuda")
+    vs = torch.empty(spanq.verify_workspace(90, 4, V), dtype=torch.uint8, device="cuda")
+    for T in (900, 257, 256, 130, 1):
+        case = _adapt_case(T, K, parts, R, S, seed=T)
+        d = [t.cuda() for t in case]
+        out = torch.empty_like(d[1])
+        spanq.adapter_apply(d[0], d[1], d[2], d[3], d[4], d[5], out, parts=parts, ranks=d[6], workspace=ws)
+        _check_adapt(out.cpu(), case, parts, f"{T} rows")
+    for n in (90, 30, 1):
+        t = torch.randn(n * 5, V, device="cuda")
+        u = torch.rand(n, 4, device="cuda")
+        acc, tok = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, 5, dtype=torch.int32, device="cuda")
+        d = t.view(n, 5, V)[:, :4].argmax(-1).to(torch.int32)
+        spanq.verify_drafts(t, d, u * 0, u[:, 0].contiguous(), None, acc, tok, workspace=vs)
+        assert bool((acc == 4).all()) and torch.equal(tok[:, :4], d)  # 0 < p keeps them all
+
+
 def test_row_operators_on_another_stream():
     """Work on a stream of its own, workspace taken there, ordered by an event alone."""
     side = torch.cuda.Stream()
@@ -466,6 +485,27 @@ def _logits(n, k, V, seed, dist):
 def test_verify(n, k, V, dist):
     target, draft, drafts, ua, us, heat = _logits(n, k, V, n + k + V, dist)
     _verify_and_check(target, draft, drafts, None, ua, us, heat, None, None, k, f"verify n {n} k {k} V {V} draft logits {dist}")
+
+
+@pytest.mark.parametrize("dist", [False, True])
+@pytest.mark.parametrize("n,k,V", [(4, 3, 511), (3, 2, 512), (5, 1, 513), (3, 2, 1025), (2, 2, 32768), (2, 2, 32769), (2, 1, 65536),
+                                   (2, 1, 65537), (300, 64, 600), (300, 64, 1030), (5, 64, 600)])
+def test_verify_chunks_of_every_size(n, k, V, dist):
+    """Vocabularies around the borders of the chunks, and calls that take another chunk for their number
+    of requests alone; of the long lists of drafts few are there, and their rows lie packed."""
+    g = _gen(n + V)
+    nd = torch.randint(0, min(k, 3) + 1, (n,), generator=g)
+    row0 = torch.cumsum(nd + 1, 0) - nd - 1
+    drow0 = torch.cumsum(nd, 0) - nd
+    target = torch.randn(int((nd + 1).sum()), V, generator=g) * 2
+    draft = torch.randn(int(nd.sum()), V, generator=g) * 2 if dist else None
+    drafts, ua, us = torch.zeros(n, k, dtype=torch.int32), torch.rand(n, k, generator=g) ** 2, torch.rand(n, generator=g)
+    for i in range(n):
+        for j in range(int(nd[i])):
+            drafts[i, j] = target[row0[i] + j].argmax() if j % 2 else torch.randint(0, V, (1,), generator=g)[0]
+    i32 = torch.int32
+    _verify_and_check(target, draft, drafts, nd.to(i32), ua, us, None, row0.to(i32), drow0.to(i32), k,
+                      f"chunks n {n} k {k} V {V} draft logits {dist}")
 
 
 @pytest.mark.parametrize("n,V", [(1, 1), (300, 5), (64, 4096), (33, 32001), (3, 128256)])

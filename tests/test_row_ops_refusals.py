@@ -105,6 +105,17 @@ def test_adapter_workspace_holds_a_partial_of_every_row_worked_at_once(lib, rows
     assert min(rows, 1 << 16) * cols * 4 <= got <= min(rows, 1 << 16) * (cols * 4 * 17 + 8)
 
 
+def test_workspaces_serve_smaller_calls():
+    sizes = [0, 1, 7, 14, 15, 28, 29, 57, 64, 65, 113, 128, 129, 192, 200, 256, 257, 300, 520, 1024, 1030, 2048, 4096,
+             4160, 9000, 16384, 16448, 65536, 65537, 65736, 70000, 131072, 1 << 20]
+    for args in ((4096, 16, (4096,)), (4096, 128, (16384, 8192, 512)), (14336, 64, (4096,)), (8, 8, (8,))):
+        need = [spanq.adapter_workspace(n, *args) for n in sizes]
+        assert need == sorted(need)
+    for args in ((0, 1000), (4, 1000), (4, 32768), (8, 50257), (64, 65536), (7, 128256), (0, 1 << 24)):
+        need = [spanq.verify_workspace(n, *args) for n in sizes]
+        assert need == sorted(need)
+
+
 def test_workspaces_refuse_sizes_of_no_call():
     for args in ((4, 60, 16, (8,)), (4, 64, 16, (12,)), (-1, 64, 16, (8,)), (4, 64, 130, (8,)), (4, 64, 16, ())):
         with pytest.raises(spanq.SpanError):

@@ -274,7 +274,7 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
       const int64_t to = h_row(row);
       const int r = (ct0 + c) % s.rank_blocks * 16 + 4 * q;  // past the rank H is zero
       sum = float4{r < rank ? sum.x : 0.f, r + 1 < rank ? sum.y : 0.f, r + 2 < rank ? sum.z : 0.f, r + 3 < rank ? sum.w : 0.f};
-      if (!kFew && s.slices == 1)
+      if (!kFew && s.h && s.slices == 1)
         store_split(s.h + 2 * (to * s.h_cols + (ct0 + c) * 16), q, sum);
       else
         *reinterpret_cast<float4*>(s.part + (slice * s.rows + to) * s.h_cols + (ct0 + c) * 16 + 4 * q) = sum;
@@ -399,20 +399,39 @@ unsigned col_blocks(const Shape& s) {
   return n;
 }
 
-// Few rows: one group, 64 columns a wave.
-constexpr int kFewJ = 4;
-__global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_few_kernel(const Shape s) {
-  constexpr int J = kFewJ;
+// One group of few rows, or a tile of 16 ordered rows of a call that has too few for runs: 64
+// columns a wave.  The slices' partials are added up on the way.  A tile's adapters are dealt to
+// kManyGroups work-groups, as in shrink.
+constexpr int kTileJ = 4;
+template <bool kFew>
+__global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(const Shape s) {
+  constexpr int J = kTileJ;
   using O = Out<J, false>;
   __shared__ int list[kTile];
   __shared__ uint2 hs[128 / 16][kTile][2][4];  // [block of ranks][row][high, low][four ranks]
   const int lane = threadIdx.x & 63;
   const int m = lane & 15, g = lane >> 4;
   const Cols cols = cols_of<J>(s, blockIdx.x, wave_id());
-  int aid = 0;
-  const int count = few_group(s, blockIdx.y, &aid, list);
   const bool in_place = s.base == s.out && s.base_stride == s.out_stride;
-  if (count == 0 || (aid < 0 && in_place)) return;
+  const int64_t row0 = static_cast<int64_t>(blockIdx.y) * kTile;  // (of the order)
+  int aid = 0, count = 0;
+  unsigned long long todo = 1;  // adapters of the tile that are this work-group's, as their first rows
+  if constexpr (kFew) {
+    count = few_group(s, blockIdx.y, &aid, list);
+    if (count == 0 || (aid < 0 && in_place)) return;
+  } else {
+    count = static_cast<int>(min<int64_t>(kTile, s.rows - row0));
+    const int2 at = lane < count ? s.order[row0 + lane] : int2{0, -1};
+    aid = at.y;
+    if (threadIdx.x < kTile) list[lane] = at.x;
+    __syncthreads();
+    todo = 0;
+    int n = 0;
+    for_adapters(aid, (1ull << count) - 1, [&](int id, unsigned long long mine) {
+      if (n++ % kManyGroups == static_cast<int>(blockIdx.z) && !(id < 0 && in_place)) todo |= mine & -mine;
+    });
+    if (todo == 0) return;
+  }
   const bool has_col = cols.n0 + J * m < cols.width;
   const bf16_t* base = s.base + cols.col0;
   bf16_t* out = s.out + cols.col0;
@@ -420,54 +439,78 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_few_kernel(c
   typename O::Vec bv[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) bv[i] = O::base(base, s.base_stride, cols, list[min(4 * g + i, count - 1)], m);
-  if (aid < 0) {
+  auto put = [&](unsigned long long mine, auto value) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (has_col && 4 * g + i < count) O::store(out, s.out_stride, cols, list[4 * g + i], m, bv[i]);
-    return;
-  }
-  // the first block's weights, asked for before its rank is known
-  uint4 wv[J];
+      if (has_col && ((mine >> (4 * g + i)) & 1)) O::store(out, s.out_stride, cols, list[4 * g + i], m, value(i));
+  };
+  // H of the rows, formed once and only if any has an adapter: eight slices' partials asked for
+  // before the first is added
+  bool formed = false;
+  auto form = [&] {
+    const int64_t plane = s.rows * s.h_cols;
+    for (int e = threadIdx.x; e < kTile * 4 * s.rank_blocks; e += 64 * kExpandWaves) {
+      const int q = e & 3, row = (e >> 2) & 15, rb = e >> 6;
+      if (row < count) {
+        const int64_t at = kFew ? list[row] : row0 + row;
+        const float4* p = reinterpret_cast<const float4*>(s.part + at * s.h_cols + (cols.part * s.rank_blocks + rb) * 16) + q;
+        float4 sum{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int j = 0; j < J; ++j) wv[j] = O::weights(s, cols, aid, j, m, 8 * (g & 1), 0, true);
-  const int rank = rank_of(s, aid);
-  const float scale = s.scale ? s.scale[aid] : 1.f;
-  // H of the group: every slice's partial asked for before the first is added
-  const int64_t plane = s.rows * s.h_cols;
-  for (int e = threadIdx.x; e < kTile * 4 * s.rank_blocks; e += 64 * kExpandWaves) {
-    const int q = e & 3, row = (e >> 2) & 15, rb = e >> 6;
-    if (row < count) {
-      const float4* p = reinterpret_cast<const float4*>(s.part + list[row] * static_cast<int64_t>(s.h_cols) +
-                                                        (cols.part * s.rank_blocks + rb) * 16) + q;
-      float4 v[kFewSlices];
+        for (int i0 = 0; i0 < (kFew ? kFewSlices : kManySlices); i0 += 8) {
+          if (i0 >= s.slices) break;
+          float4 v[8];
 #pragma unroll
-      for (int i = 0; i < kFewSlices; ++i) v[i] = i < s.slices ? p[i * plane / 4] : float4{0.f, 0.f, 0.f, 0.f};
-      float4 sum = v[0];
+          for (int i = 0; i < 8; ++i) v[i] = i0 + i < s.slices ? p[(i0 + i) * plane / 4] : float4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 1; i < kFewSlices; ++i) sum = sum + v[i];
-      store_split(reinterpret_cast<bf16_t*>(hs[rb][row]), q, sum);
+          for (int i = 0; i < 8; ++i) sum = sum + v[i];
+        }
+        store_split(reinterpret_cast<bf16_t*>(hs[rb][row]), q, sum);
+      }
     }
-  }
-  __syncthreads();
-  f32x4_t acc[J] = {};
-  for (int rb = 0; 16 * rb < rank; ++rb) {
-    const uint4 hv = *reinterpret_cast<const uint4*>(&hs[rb][min(m, count - 1)][g >> 1][2 * (g & 1)]);
-    if (16 * rb + 16 > rank) {
-#pragma unroll
-      for (int j = 0; j < J; ++j) wv[j] = first_of(wv[j], rank - 16 * rb - 8 * (g & 1));
+    __syncthreads();
+  };
+  while (todo) {
+    const int lead = __ffsll(todo) - 1;
+    todo &= todo - 1;
+    unsigned long long mine = (1ull << count) - 1;
+    if constexpr (!kFew) {
+      const int id = __builtin_amdgcn_readlane(aid, lead);
+      mine = __ballot(lane < count && aid == id);
+      if (id < 0) {
+        put(mine, [&](int i) { return bv[i]; });
+        continue;
+      }
+    } else if (aid < 0) {
+      put(mine, [&](int i) { return bv[i]; });
+      return;
     }
-    uint4 next[J];
+    const int id = kFew ? aid : __builtin_amdgcn_readlane(aid, lead);
+    // the first block's weights, asked for before its rank is known
+    uint4 wv[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) next[j] = O::weights(s, cols, aid, j, m, 16 * (rb + 1) + 8 * (g & 1), 0, true);
+    for (int j = 0; j < J; ++j) wv[j] = O::weights(s, cols, id, j, m, 8 * (g & 1), 0, true);
+    const int rank = rank_of(s, id);
+    const float scale = s.scale ? s.scale[id] : 1.f;
+    if (!formed) form();
+    formed = true;
+    f32x4_t acc[J] = {};
+    for (int rb = 0; 16 * rb < rank; ++rb) {
+      const uint4 hv = *reinterpret_cast<const uint4*>(&hs[rb][min(m, count - 1)][g >> 1][2 * (g & 1)]);
+      if (16 * rb + 16 > rank) {
 #pragma unroll
-    for (int j = 0; j < J; ++j)
-      acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(hv), as_frag(wv[j]), acc[j], 0, 0, 0);
+        for (int j = 0; j < J; ++j) wv[j] = first_of(wv[j], rank - 16 * rb - 8 * (g & 1));
+      }
+      uint4 next[J];
 #pragma unroll
-    for (int j = 0; j < J; ++j) wv[j] = next[j];
+      for (int j = 0; j < J; ++j) next[j] = O::weights(s, cols, id, j, m, 16 * (rb + 1) + 8 * (g & 1), 0, true);
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(hv), as_frag(wv[j]), acc[j], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < J; ++j) wv[j] = next[j];
+    }
+    put(mine, [&](int i) { return O::add(bv[i], acc, i, scale); });
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (has_col && 4 * g + i < count) O::store(out, s.out_stride, cols, list[4 * g + i], m, O::add(bv[i], acc, i, scale));
 }
 
 // Many rows: 64 columns a wave, a run of tiles of 16 rows one after another.  The next tile's
@@ -603,7 +646,15 @@ unsigned h_groups(const Shape& s) {
 // many in us, 1 adapter and 32 mixed ones:
 //   N 4096, rank 16:   130 rows 15.0 / 14.4, 10.0 / 30.7   256 rows 20.2 / 14.6, 12.8 / 21.1
 //   N 28672, rank 32:   96 rows 25.7 / 19.1, 39.7 / 55.8   192 rows 42.7 / 22.1, 54.1 / 46.5
-int few_rows(const Shape& s) { return s.N <= 8192 ? kFewRows : kFewRows / 2; }
+constexpr int kNarrow = 8192;
+int few_rows(const Shape& s) { return s.N <= kNarrow ? kFewRows : kFewRows / 2; }
+
+// Many rows, but too few for runs: their expand adds the slices' partials up itself, up to so
+// many blocks of 16 ranks of them for a row, a launch less; every work-group across the columns does
+// it again.  Itself / by a launch, us:
+//   N 4096, rank 16:   257 rows 13.4 / 15.8, 384 rows of 32 mixed adapters 20.9 / 24.0
+//   N 28672, rank 32:  130 rows 24.5 / 21.5, 32 mixed adapters 68.7 / 55.4
+constexpr int kTilePartials = 32;
 
 // `rows` rows of the call from `first` on; *bytes: of the workspace they need.
 Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows, size_t* bytes) {
@@ -636,14 +687,14 @@ Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows, size_t* 
   const int64_t n = std::max<int64_t>(1, std::min(want, most));
   s.k_slice = static_cast<int>(((s.K + n - 1) / n + unit - 1) / unit * unit);
   s.slices = (s.K + s.k_slice - 1) / s.k_slice;
-  const int64_t planes = few || s.slices > 1 ? s.slices : 0;
   // runs as long as leave two work-groups for a CU
   s.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kManyRun, (rows + 15) / 16 * col_blocks<kManyJ>(s) / 512)));
+  const bool tile = few || (s.run == 1 && s.N <= kNarrow && s.slices * s.rank_blocks <= kTilePartials);
+  const int64_t plane = rows * s.h_cols, planes = tile || s.slices > 1 ? s.slices : 0;
   s.part = static_cast<float*>(c.workspace);
-  s.h = reinterpret_cast<bf16_t*>(s.part + planes * rows * s.h_cols);
-  s.order = reinterpret_cast<int2*>(s.part + (planes + 1) * rows * s.h_cols);
-  *bytes = few ? planes * rows * s.h_cols * sizeof(float)
-               : (planes + 1) * rows * s.h_cols * sizeof(float) + rows * sizeof(int2);
+  s.h = tile ? nullptr : reinterpret_cast<bf16_t*>(s.part + planes * plane);
+  s.order = few ? nullptr : reinterpret_cast<int2*>(s.part + (planes + !tile) * plane);
+  *bytes = (planes + !tile) * plane * sizeof(float) + (few ? 0 : rows * sizeof(int2));
   return s;
 }
 
@@ -687,7 +738,7 @@ hipError_t launch_adapter_apply(const span_adapter_call& a, hipStream_t st) {
       adapter_shrink_kernel<true, FewShrink><<<dim3(s.slices * h_groups<FewShrink>(s), rows), 64 * FewShrink::kWaves, 0, st>>>(s);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
-      adapter_expand_few_kernel<<<dim3(col_blocks<kFewJ>(s), rows), 64 * kExpandWaves, 0, st>>>(s);
+      adapter_expand_tile_kernel<true><<<dim3(col_blocks<kTileJ>(s), rows), 64 * kExpandWaves, 0, st>>>(s);
     } else {
       const unsigned tiles = static_cast<unsigned>((s.rows + 16 * kManyTiles - 1) / (16 * kManyTiles));
       adapter_order_kernel<<<1, kOrderThreads, 0, st>>>(s);
@@ -695,13 +746,16 @@ hipError_t launch_adapter_apply(const span_adapter_call& a, hipStream_t st) {
       if (e != hipSuccess) return e;
       adapter_shrink_kernel<false, ManyShrink><<<dim3(s.slices * h_groups<ManyShrink>(s), tiles, kManyGroups), 64 * ManyShrink::kWaves, 0, st>>>(s);
       e = hipGetLastError();
-      if (e == hipSuccess && s.slices > 1) {
+      if (e == hipSuccess && s.h && s.slices > 1) {
         adapter_finish_kernel<<<static_cast<unsigned>((s.rows * s.h_cols / 4 + 255) / 256), 256, 0, st>>>(s);
         e = hipGetLastError();
       }
       if (e != hipSuccess) return e;
       const unsigned runs = static_cast<unsigned>((s.rows + 16 * s.run - 1) / (16 * s.run));
-      adapter_expand_many_kernel<<<dim3(col_blocks<kManyJ>(s), runs), 64 * kExpandWaves, 0, st>>>(s);
+      if (s.h)
+        adapter_expand_many_kernel<<<dim3(col_blocks<kManyJ>(s), runs), 64 * kExpandWaves, 0, st>>>(s);
+      else
+        adapter_expand_tile_kernel<false><<<dim3(col_blocks<kTileJ>(s), runs, kManyGroups), 64 * kExpandWaves, 0, st>>>(s);
     }
     e = hipGetLastError();
     if (e != hipSuccess) return e;

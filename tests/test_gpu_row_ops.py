@@ -217,6 +217,21 @@ def test_adapters_long_reductions_large_ranks_odd_widths(T, K, parts, R, S):
     _check_adapt(out.cpu(), case, parts, "out")
 
 
+@pytest.mark.parametrize("T,K,parts,R,S", [(200, 2048, (8200, 1000), 24, 5), (600, 4096, (264,), 128, 3), (1031, 520, (4104,), 40, 4),
+                                           (1100, 2048, (8, 8200), 16, 2), (2100, 264, (4096,), 8, 30)])
+def test_adapters_of_many_rows_and_columns(T, K, parts, R, S):
+    """Wide products, large ranks and runs of tiles: mixed rows, and segments."""
+    for ids in (None, [i * S // T - (i % 97 == 5) for i in range(T)]):
+        case = _adapt_case(T, K, parts, R, S, seed=T + R, ids=ids)
+        print(f"adapters T {T} K {K} parts {parts} R {R} S {S}", flush=True)
+        d = [t.cuda() for t in case]
+        out = torch.empty_like(d[1])
+        spanq.adapter_apply(d[0], d[1], d[2], d[3], d[4], d[5], out, parts=parts, ranks=d[6])
+        _check_adapt(out.cpu(), case, parts, "out")
+        spanq.adapter_apply(d[0], d[1], d[2], d[3], d[4], d[5], d[1], parts=parts, ranks=d[6])  # in place
+        assert torch.equal(d[1], out)
+
+
 @pytest.mark.parametrize("T", [40, 300])
 def test_adapters_strides_ids_outside_and_no_adapter_at_all(T):
     parts, S = (72, 16), 3

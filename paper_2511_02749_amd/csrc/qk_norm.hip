@@ -5,7 +5,8 @@
 //   at angle  position * theta^(-2i/d)
 //
 // and the rows' way from one product's q|k|v rows to the caller's rows; values are copied.
-// Bound: HBM, each element read once and written once, ~10 operations each.
+// Bound: HBM, each element read once and written once, ~10 operations each.  8192 rows of 32 + 2 x 8
+// heads of 128 with their rotation take 39 us, 5.2 TB/s, as fast as a copy; one row 3 us.
 //
 // A lane holds 16 bytes of the head's first half and the 16 bytes d/2 further on, so both
 // members of a pair are in one lane, the sum of squares takes log2(lanes per head) lane

@@ -27,6 +27,9 @@ def _need_gpu():
     if not torch.cuda.is_available():
         pytest.skip("no GPU")
     print(flush=True)
+    yield
+    if torch.cuda.memory_reserved() > 8 << 30:  # for the pools of other tests
+        torch.cuda.empty_cache()
 
 
 def _gen(seed):
@@ -678,3 +681,91 @@ def test_a_call_leaves_the_current_device_and_refuses_tensors_of_the_wrong_kind(
                  (lg, tok[:, :1].contiguous(), u[:, None], u, None, i.long(), tok)):
         with pytest.raises(spanq.SpanError):
             spanq.verify_drafts(*args)
+
+
+# ------------------------------------------------------------------------ the largest sizes
+
+def _far(rows, width, stride, dtype):
+    """Rows of a buffer that is not filled in between them, `stride` elements apart."""
+    return torch.empty(rows * stride, dtype=dtype, device="cuda").as_strided((rows, width), (stride, 1))
+
+
+@pytest.mark.parametrize("T", [200, 300])
+def test_adapters_rows_far_apart(T):
+    """Offsets of x past 2^32 elements, of base and out past 2^32 bytes."""
+    case = _adapt_case(T, 136, (72,), 16, 3, seed=T)
+    d = [t.cuda() for t in case]
+    x, out = _far(T, 136, 1 << 25, torch.bfloat16), _far(T, 72, 1 << 23, torch.bfloat16)
+    x.copy_(d[0])
+    out.copy_(d[1])
+    print(f"{T} rows, {x.stride(0) * T * 2 >> 30} GiB of x", flush=True)
+    spanq.adapter_apply(x, out, d[2], d[3], d[4], d[5], out, ranks=d[6])
+    _check_adapt(out.cpu(), case, (72,), "far apart")
+
+
+@pytest.mark.parametrize("T", [3, 140])
+def test_adapters_of_the_widest_products(T):
+    g = torch.Generator(device="cuda").manual_seed(T)
+    N, R, S, K = 1 << 20, 24, 3, 64
+    def randn(*shape):
+        return torch.randn(*shape, generator=g, device="cuda", dtype=torch.bfloat16)
+    x, out, a, b = randn(T, K), randn(T, N), randn(S, 1, R, K) / 8, randn(S, N, R)
+    ids = torch.randint(-1, S, (T,), generator=g, device="cuda", dtype=torch.int32)
+    base, cols = out.clone(), torch.cat([torch.arange(64), torch.arange(N // 2 - 32, N // 2 + 32), torch.arange(N - 64, N)]).cuda()
+    print(f"{T} rows of {N} columns", flush=True)
+    spanq.adapter_apply(x, out, ids, a, b, None, out)
+    case = [t.cpu() for t in (x, base[:, cols], ids, a, b[:, cols], torch.ones(S), torch.full((S,), R))]
+    _check_adapt(out[:, cols].cpu(), case, (len(cols),), "widest")
+
+
+def test_adapters_of_the_longest_reduction():
+    case = _adapt_case(5, 1 << 20, (8,), 8, 2, seed=20)
+    d = [t.cuda() for t in case]
+    out = torch.empty_like(d[1])
+    spanq.adapter_apply(d[0], d[1], d[2], d[3], d[4], d[5], out, ranks=d[6])
+    _check_adapt(out.cpu(), case, (8,), "K 2^20")
+
+
+@pytest.mark.parametrize("dist", [False, True])
+def test_verify_of_the_largest_vocabulary(dist):
+    n, k, V = 1, 1, 1 << 24
+    target, draft, drafts, ua, us, _ = _logits(n, k, V, 24, dist)
+    for u in (0.0, 0.9999999):  # kept, or refused
+        _verify_and_check(target, draft, drafts, None, ua * 0 + u, us, None, None, None, k, f"V 2^24, draft logits {dist}, u {u}")
+
+
+def test_verify_rows_far_apart():
+    n, k, V = 2, 2, 600
+    target, draft, drafts, ua, us, heat = _logits(n, k, V, 5, True)
+    t, y = _far(n * (k + 1), V, 1 << 29, torch.float32), _far(n * k, V, 1 << 30, torch.float32)
+    t.copy_(target)
+    y.copy_(draft)
+    _verify_and_check(target, draft, drafts, None, ua, us, heat, None, None, k, "far apart", t, y)
+
+
+def test_head_norms_far_apart_and_of_many_heads_in_a_graph():
+    """Strides past 2^32 bytes, more heads than a work-group has threads; captured, with positions and rows
+    that change between the replays."""
+    n, hq, hkv, dim, far = 3, 517, 70, 64, 1 << 31
+    g = _gen(9)
+    x, kv = torch.randn(n, hq, dim, generator=g).to(torch.bfloat16), torch.randn(n, hkv, dim, generator=g).to(torch.bfloat16)
+    gain = (1 + 0.3 * torch.randn(dim, generator=g)).to(torch.bfloat16)
+    q = torch.empty((n - 1) * far + hq * dim, dtype=torch.bfloat16, device="cuda").as_strided((n, hq, dim), (far, dim, 1))
+    q.copy_(x.cuda())
+    k, gd = kv.cuda(), gain.cuda()
+    qo = torch.zeros((n, hq, dim), dtype=torch.bfloat16, device="cuda")
+    ko = torch.zeros((n, hkv, dim), dtype=torch.bfloat16, device="cuda")
+    pos, rows = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.arange(n, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        spanq.qk_norm_rope(q, k, None, gd, gd, 1e-5, qo, ko, None, rows=rows, positions=pos)
+    for step in range(3):
+        at = torch.randint(0, 1 << 20, (n,), generator=g).to(torch.int32)
+        to = torch.randperm(n, generator=g)
+        pos.copy_(at)
+        rows.copy_(to.to(torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        _check_heads(qo.cpu()[to], x, gain, 1e-5, at, 1e4, f"q, replay {step}")
+        _check_heads(ko.cpu()[to], kv, gain, 1e-5, at, 1e4, f"k, replay {step}")

@@ -46,8 +46,10 @@ def _rows(who: str, name: str, t, dtype, index: int, shape):
     """(address, row stride) of a [rows, width] or [rows, heads, dim] tensor of that shape whose rows are dense."""
     if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
         raise _bad(who, f"{name} must be {dtype} {tuple(shape)} on GPU {index}, not {t.dtype} {tuple(t.shape)} on {t.device}")
-    stride = t.stride()
     width = shape[-1]
+    if t.is_contiguous():  # (asked first: strides cost more than this)
+        return t.data_ptr(), width * shape[1] if len(shape) == 3 else width
+    stride = t.stride()
     if stride[-1] != 1 and width > 1:
         raise _bad(who, f"the elements of a row of {name} must follow one another")
     if len(stride) == 3:

@@ -18,8 +18,8 @@
 //
 // Weights and sums are 64-bit: borders of the running sum over 10^5 tokens lie 10^-5 and
 // less apart, where 32-bit sums, and their order, would choose another token every few
-// thousand calls.  64-bit instructions run at the 32-bit rate here; the exponential is the
-// Taylor series of 2^f on [-1/2, 1/2] to the 11th power (6e-15 relative), without a branch.
+// thousand calls.  64-bit instructions run at the 32-bit rate here; an exponential
+// takes 17 of them.
 //
 // Bound: HBM, each logit read once (and the deciding row again, from the last-level cache),
 // about 20 vector instructions per logit beside it.  64 requests of 4 drafts with a distribution,
@@ -42,7 +42,7 @@ constexpr int kMaxDrafts = SPAN_MAX_DRAFTS;
 constexpr double kLog2e = 1.4426950408889634074;
 
 struct Stat {
-  double sum;  // of exp((x - max) / T) over the chunk
+  double sum;  // of the weights, relative to the chunk's own largest logit (scale_of)
   float max;   // -inf: nothing in the chunk has weight
   int32_t arg;
 };
@@ -56,31 +56,39 @@ struct Args {
   double* left;    // [requests][chunks]: sums of max(p - q, 0)
 };
 
-// 2^t for t <= 0 (and up to 1); 0 for -inf and NaN, whose bound, 2^-1200, underflows.
-__device__ __forceinline__ double exp2_neg(double t) {
-  t = fmax(t, -1200.0);
-  const double k = rint(t), f = t - k;
-  // ln(2)^n / n!
-  double p = 4.4455382718708114976e-10;
-  p = fma(p, f, 7.0549116208011233299e-9);
-  p = fma(p, f, 1.0178086009239699728e-7);
-  p = fma(p, f, 1.3215486790144309488e-6);
-  p = fma(p, f, 1.5252733804059840280e-5);
-  p = fma(p, f, 1.5403530393381609954e-4);
-  p = fma(p, f, 1.3333558146428443423e-3);
-  p = fma(p, f, 9.6181291076284771620e-3);
-  p = fma(p, f, 5.5504108664821579953e-2);
-  p = fma(p, f, 2.4022650695910071233e-1);
-  p = fma(p, f, 6.9314718055994530942e-1);
-  p = fma(p, f, 1.0);
-  return ldexp(p, static_cast<int>(k));
+// What weights are relative to: w(x) = 2^(x c - k), c = log2(e) / T, k the whole number next to c
+// times the largest logit, so that x c - k is rounded once.  Where that logit is infinite, or c times
+// it past 2^40, all the weight lies on the logits equal to it (others, 2^-24 of it away, weigh
+// nothing); where it is -inf, there is none.
+struct Scale {
+  double c, k;
+  float only;  // `hot`: the logit with all the weight, NaN if none has any
+  bool hot;
+};
+__device__ __forceinline__ Scale scale_of(float max, double c) {
+  const double at = static_cast<double>(max) * c;
+  return Scale{c, rint(at), max > -INFINITY ? max : NAN, !(fabs(at) < 0x1p40)};
 }
 
-// The weight of logit x against the row's (or chunk's) largest one, c = log2(e) / T: 1 at it
-// (an infinite one too), else exp((x - max) / T); 0 for -inf and NaN.
-__device__ __forceinline__ double weight(float x, float max, double c) {
-  const double w = exp2_neg((static_cast<double>(x) - static_cast<double>(max)) * c);
-  return max > -INFINITY ? (x == max ? 1.0 : w) : 0.0;
+// 2^t of t = x c - k, c and k finite; 0 below 2^-1200, which -inf and NaN are taken to.
+__device__ __forceinline__ double weight_at(float x, const Scale& s) {
+  const double t = fmax(fma(static_cast<double>(x), s.c, -s.k), -1200.0);
+  const double n = rint(t), f = t - n;
+  // 2^f on [-1/2, 1/2], least relative error of a polynomial (Remez exchange): 1.36e-14
+  double p = 1.0150337260976417e-07;
+  p = fma(p, f, 1.3259405611204192e-06);
+  p = fma(p, f, 1.5252984835578367e-05);
+  p = fma(p, f, 1.5403434948081424e-04);
+  p = fma(p, f, 1.3333557617609879e-03);
+  p = fma(p, f, 9.6181291920672020e-03);
+  p = fma(p, f, 5.5504108668685580e-02);
+  p = fma(p, f, 2.4022650695649653e-01);
+  p = fma(p, f, 6.9314718055987100e-01);
+  p = fma(p, f, 1.0000000000000127);
+  return ldexp(p, static_cast<int>(n));
+}
+__device__ __forceinline__ double weight(float x, const Scale& s) {
+  return s.hot ? (x == s.only ? 1.0 : 0.0) : weight_at(x, s);
 }
 
 // Values of other lanes by vector instructions alone: DPP rotations inside a row of 16, and
@@ -221,13 +229,13 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(const Args a) {
     arg = wave_min(arg);
   }
   double sum = 0.0;
-  if (best == INFINITY) {  // all the weight on the infinite ones
+  const Scale s = scale_of(best, r.c);
+  if (s.hot) {
 #pragma unroll
-    for (int u = 0; u < kPer; ++u) sum += x[u] == best ? 1.0 : 0.0;
-  } else if (best > -INFINITY) {
-    const double max = best;
+    for (int u = 0; u < kPer; ++u) sum += x[u] == s.only ? 1.0 : 0.0;
+  } else {
 #pragma unroll
-    for (int u = 0; u < kPer; ++u) sum += exp2_neg((static_cast<double>(x[u]) - max) * r.c);
+    for (int u = 0; u < kPer; ++u) sum += weight_at(x[u], s);
   }
   sum = wave_sum(sum);
   if (lane == 0) {
@@ -235,6 +243,13 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(const Args a) {
                      : a.target + (static_cast<int64_t>(q) * (k + 1) + j) * a.chunks;
     to[chunk] = Stat{sum, best, arg};
   }
+}
+
+// What a chunk's sum is in the row's scale.
+__device__ __forceinline__ double in_row(const Stat& chunk, const Scale& row) {
+  if (row.hot) return chunk.max == row.only ? chunk.sum : 0.0;
+  const double octaves = rint(static_cast<double>(chunk.max) * row.c) - row.k;
+  return ldexp(chunk.sum, static_cast<int>(fmax(octaves, -3000.0)));
 }
 
 // A row's largest logit, its lowest id (greedy requests) and its sum of weights, by one wave;
@@ -252,8 +267,9 @@ __device__ __forceinline__ Stat whole_row(const Stat* st, int chunks, const Requ
       if (st[i].max == best) arg = min(arg, st[i].arg);
     arg = wave_min(arg);
   }
-  double sum = *own = mine.sum * weight(mine.max, best, r.c);
-  for (int i = lane + 64; i < chunks; i += 64) sum += st[i].sum * weight(st[i].max, best, r.c);
+  const Scale s = scale_of(best, r.c);
+  double sum = *own = in_row(mine, s);
+  for (int i = lane + 64; i < chunks; i += 64) sum += in_row(st[i], s);
   return Stat{wave_sum(sum), best, arg};
 }
 
@@ -303,9 +319,9 @@ __device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Ve
     if (r.greedy) {
       keep = v.p[j].sum > 0.0 && d == v.p[j].arg;
     } else if (d >= 0 && d < c.vocab) {
-      const double pd = v.p[j].sum > 0.0 ? weight(x, v.p[j].max, r.c) / v.p[j].sum : 0.0;
+      const double pd = v.p[j].sum > 0.0 ? weight(x, scale_of(v.p[j].max, r.c)) / v.p[j].sum : 0.0;
       double qd = 1.0;
-      if (dist) qd = v.q[j].sum > 0.0 ? weight(y, v.q[j].max, r.c) / v.q[j].sum : 0.0;
+      if (dist) qd = v.q[j].sum > 0.0 ? weight(y, scale_of(v.q[j].max, r.c)) / v.q[j].sum : 0.0;
       keep = static_cast<double>(u) * qd < pd;
     }
     v.keep[j] = keep;
@@ -324,12 +340,12 @@ __device__ __forceinline__ double inverse(double s) { return s > 0.0 ? 1.0 / s :
 struct Left {
   const float* x;
   const float* y;  // the draft's logits, or null
-  float pm, qm;
-  double ps, qs, c;  // 1 / sums
-  int one_hot;       // the token taken out of p where the draft has no distribution, -1: none
+  Scale p, q;
+  double ps, qs;  // 1 / sums
+  int one_hot;    // the token taken out of p where the draft has no distribution, -1: none
   __device__ __forceinline__ double of(int i, float xi, float yi) const {
-    double w = weight(xi, pm, c) * ps;
-    if (y) w = fmax(w - weight(yi, qm, c) * qs, 0.0);
+    double w = weight(xi, p) * ps;
+    if (y) w = fmax(w - weight(yi, q) * qs, 0.0);
     return i == one_hot ? 0.0 : w;
   }
 };
@@ -339,14 +355,13 @@ __device__ __forceinline__ Left left_of(const Args& a, int q, const Request& r, 
   const span_verify_call& c = a.c;
   Left l{};
   l.x = c.target_logits + (r.target_row + n) * c.target_stride;
-  l.pm = v.p[n].max;
+  l.p = scale_of(v.p[n].max, r.c);
   l.ps = inverse(v.p[n].sum);
-  l.c = r.c;
   l.one_hot = -1;
   if (n < r.n_drafts && !plain) {
     if (c.draft_logits) {
       l.y = c.draft_logits + (r.draft_row + n) * c.draft_stride;
-      l.qm = v.q[n].max;
+      l.q = scale_of(v.q[n].max, r.c);
       l.qs = inverse(v.q[n].sum);
     } else {
       const int d = v.d[n];
@@ -378,8 +393,14 @@ __global__ __launch_bounds__(kThreads) void verify_left_kernel(const Args a) {
   load_chunk(l.x, base, lane, c.vocab, x);
   load_chunk(l.y, base, lane, c.vocab, y);
   double sum = 0.0;
+  if (l.p.hot || l.q.hot) {
 #pragma unroll
-  for (int u = 0; u < kPer; ++u) sum += l.of(-2, x[u], y[u]);
+    for (int u = 0; u < kPer; ++u) sum += l.of(-2, x[u], y[u]);
+  } else {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u)
+      sum += fmax(weight_at(x[u], l.p) * l.ps - weight_at(y[u], l.q) * l.qs, 0.0);
+  }
   sum = wave_sum(sum);
   if (lane == 0) a.left[static_cast<int64_t>(q) * a.chunks + chunk] = sum;
 }
@@ -432,8 +453,8 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
       auto chunk_sum = [&](int i) -> double {
         if (i >= a.chunks) return 0.0;
         if (l.y) return a.left[static_cast<int64_t>(q) * a.chunks + i];
-        double s = (i < 64 ? s_chunk[n][i] : st[i].sum * weight(st[i].max, l.pm, l.c)) * l.ps;
-        if (l.one_hot >= 0 && l.one_hot / kChunk == i) s -= weight(v.x[n], l.pm, l.c) * l.ps;
+        double s = (i < 64 ? s_chunk[n][i] : in_row(st[i], l.p)) * l.ps;
+        if (l.one_hot >= 0 && l.one_hot / kChunk == i) s -= weight(v.x[n], l.p) * l.ps;
         return s > 0.0 ? s : 0.0;
       };
       const double own = chunk_sum(lane);  // all of them up to 64 chunks
@@ -501,8 +522,9 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
       float lp = 0.f;
       if (t >= 0) {
         const float x = j < n ? v.x[j] : r.greedy ? v.p[n].max : s_x;
-        // the largest logit (an infinite one too) has no difference to scale
-        const double d = x == v.p[j].max ? 0.0 : (static_cast<double>(x) - static_cast<double>(v.p[j].max)) * r.c;
+        const Scale s = scale_of(v.p[j].max, r.c);
+        // (a logit with all the weight is relative to itself)
+        const double d = s.hot ? 0.0 : fma(static_cast<double>(x), s.c, -s.k);
         lp = static_cast<float>(d * 0.69314718055994530942 - log(v.p[j].sum));
       }
       lps[j] = lp;

@@ -22,8 +22,9 @@
 // takes 17 of them.
 //
 // Bound: HBM, each logit read once (and the deciding row again, from the last-level cache),
-// about 20 vector instructions per logit beside it.  64 requests of 4 drafts with a distribution,
-// 128256 tokens (295 MB): 64 us in 1 (4.6 TB/s), 24 in 2, 10 in 3.
+// 17 vector instructions per logit beside it.  64 requests of 4 drafts with a distribution,
+// 128256 tokens (295 MB): 56 us in 1 (5.3 TB/s), 18 in 2, 10 in 3.  The instructions still count: with
+// three more for each exponential 64 and 24.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -375,8 +376,8 @@ __device__ __forceinline__ Left left_of(const Args& a, int q, const Request& r, 
 
 // ------------------------------------------------------------------ 2: what the deciding row leaves
 // All waves of 64 requests stand on the chip at once, so acceptance (5 us), their loads (66 MB) and
-// two exponentials a token (10 us of instructions) follow one another: 24 us.  With 16 waves a
-// work-group 27; with acceptance in a launch of its own 21 + 5.
+// two exponentials a token (7 us of instructions) follow one another: 18 us.  With eight waves a
+// work-group the same, with 16 an eighth more; acceptance in a launch of its own costs what it saves.
 template <int kChunk>
 __global__ __launch_bounds__(kThreads) void verify_left_kernel(const Args a) {
   constexpr int kPer = kChunk / 64;
@@ -408,7 +409,7 @@ __global__ __launch_bounds__(kThreads) void verify_left_kernel(const Args a) {
 }
 
 // ------------------------------------------------------------------ 3: the token
-// 7 us for one request: five loads that need one another's results.
+// 6.5 us for one request: four loads that need one another's results, and sums over a work-group.
 template <int kChunk>
 __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a) {
   constexpr int kPickWaves = kPickThreads / 64;
@@ -540,8 +541,8 @@ int64_t chunks_of(int vocab, int chunk) { return (vocab + chunk - 1) / chunk; }
 // Logits of a chunk: the fewest of 512, 1024 and 2048 that leave a row at most 64 chunks, one for
 // each lane that adds them up, and all rows at most 2^16.  Small chunks spread few logits over the chip,
 // and are more to add up in 2 and 3.  Four drafts with a distribution, captured calls of 512 / 1024 / 2048 in us:
-//   vocabulary 8000:    8 requests 15.8 / 18.6 / 22.6   64: 22.2 / 24.4 / 27.9   256: 36.5 / 36.2 / 39.5
-//   vocabulary 32768:   8 requests 17.1 / 19.0 / 23.0   64: 34.4 / 34.2 / 35.1   256: 107 / 94 / 89
+//   vocabulary 8000:    8 requests 15.2 / 16.7 / 20.1   64: 21.0 / 22.2 / 25.1   256: 34.2 / 33.4 / 35.9
+//   vocabulary 32768:   8 requests 15.9 / 17.0 / 20.6   64: 32.3 / 31.5 / 32.2   256: 100 / 88 / 83
 bool chunk_fits(int64_t requests, int max_drafts, int vocab, int chunk) {
   const int64_t n = chunks_of(vocab, chunk);
   return n <= 64 && requests * (2 * max_drafts + 1) * n <= 1 << 16;

@@ -156,7 +156,7 @@ __device__ __forceinline__ float4 operator+(const float4& a, const float4& b) {
 // the number of the others' buckets lie among each other, which costs time, nothing else).  One
 // work-group counts each bucket's rows, adds the counts up and gives every row its place; which
 // of a bucket's rows comes first may change from run to run, and no result depends on it.
-// 777 rows 4.1 us, 2048 rows 5.0: the latency of two passes.  Without it 2048 rows of 32 mixed
+// 777 rows 4.1 us, 2048 rows 4.8, 65536 rows 38 to 50: the latency of two passes.  Without it 2048 rows of 32 mixed
 // adapters (rank 32, 4096 -> 28672) take 1002 us for 95, and rows in segments 4 us less.
 constexpr int kOrderThreads = 1024;  // and buckets
 __global__ __launch_bounds__(kOrderThreads) void adapter_order_kernel(const Shape s) {
@@ -175,9 +175,21 @@ __global__ __launch_bounds__(kOrderThreads) void adapter_order_kernel(const Shap
     if (before == 0) at = atomicAdd(&place[bucket], __popcll(all));
     return __builtin_amdgcn_readfirstlane(at) + before;
   };
+  // f(row, its adapter) for the thread's rows, four ids asked for together
+  auto each = [&](auto f) {
+    constexpr int kAhead = 4;
+    for (int i0 = t; i0 < n; i0 += kAhead * kOrderThreads) {
+      int id[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) id[u] = adapter_of(s, i0 + u * kOrderThreads);
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+        if (i0 + u * kOrderThreads < n) f(i0 + u * kOrderThreads, id[u]);
+    }
+  };
   place[t] = 0;
   __syncthreads();
-  for (int i = t; i < n; i += kOrderThreads) take(adapter_of(s, i));
+  each([&](int, int id) { take(id); });
   __syncthreads();
   const int mine = place[t];
   int upto = mine;  // sum of the wave's buckets up to this one
@@ -192,10 +204,7 @@ __global__ __launch_bounds__(kOrderThreads) void adapter_order_kernel(const Shap
   for (int w = 0; w < wave_id(); ++w) before += sums[w];
   place[t] = before;
   __syncthreads();
-  for (int i = t; i < n; i += kOrderThreads) {
-    const int id = adapter_of(s, i);
-    s.order[take(id)] = int2{i, id};
-  }
+  each([&](int i, int id) { s.order[take(id)] = int2{i, id}; });
 }
 
 // H of one group (few) or of a tile of 64 ordered rows: one slice of K, C::kCols column tiles.

@@ -181,7 +181,7 @@ def load():
         "span_model_set_adapters": (I32, [VP, P(ModelAdapters)]),
         "span_model_decode_drafts": (I32, [VP, VP, P(I32), P(I32), P(I32), I32, P(Sampling), P(I32), P(I32),
                                            P(ctypes.c_float), VP]),
-        # argument records packed by row_ops.py
+        # argument records as bytes
         "span_qk_norm_rope": (I32, [ctypes.c_char_p, VP]),
         "span_adapter_workspace": (I32, [ctypes.c_char_p, P(ctypes.c_size_t)]),
         "span_adapter_apply": (I32, [ctypes.c_char_p, VP]),

@@ -1,4 +1,5 @@
-"""Build the HIP library (libspanq.so) in-tree for gfx950.
+"""Build the HIP library (libspanq.so) in-tree for gfx950, and the native part of the torch
+binding of the row operators (_rowops.so).
 
 Every source is compiled on each call (hipcc cross-compiles without a GPU),
 objects in parallel, then linked into ``paper_2511_02749_amd/libspanq.so``.
@@ -6,14 +7,18 @@ objects in parallel, then linked into ``paper_2511_02749_amd/libspanq.so``.
 from __future__ import annotations
 
 import os
+import importlib.util
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libspanq.so")
+BINDING = os.path.join(HERE, "binding", "rowops.cpp")
+BINDING_OUT = os.path.join(HERE, "_rowops.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
@@ -43,13 +48,35 @@ def _compile(src: str, obj: str) -> None:
         print(err, file=sys.stderr)
 
 
+def build_binding() -> None:
+    """The torch binding (host code only); a machine without torch has no tensors to bind."""
+    if importlib.util.find_spec("torch") is None:
+        return
+    import torch
+    base = os.path.dirname(torch.__file__)
+    tmp = BINDING_OUT + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include"),
+           "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(base, "include"),
+           "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"), BINDING, "-o", tmp,
+           "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError("binding failed:\n" + r.stdout + r.stderr)
+    if r.stderr.strip():
+        print(r.stderr, file=sys.stderr)
+    os.replace(tmp, BINDING_OUT)
+
+
 def build(verbose: bool = True) -> str:
     objdir = os.path.join(HERE, "_build")
     os.makedirs(objdir, exist_ok=True)
     srcs = sources()
     objs = [os.path.join(objdir, os.path.basename(s) + ".o") for s in srcs]
-    with ThreadPoolExecutor(max_workers=min(8, len(srcs))) as ex:
+    with ThreadPoolExecutor(max_workers=min(8, len(srcs) + 1)) as ex:
+        binding = ex.submit(build_binding)
         list(ex.map(lambda so: _compile(*so), zip(srcs, objs)))
+        binding.result()
     tmp = OUT + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp, "-L/opt/rocm/lib", "-lhipblaslt",
            "-Wl,-rpath,/opt/rocm/lib"]

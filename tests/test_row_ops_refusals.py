@@ -4,12 +4,14 @@ with SPAN_EINVAL, before any HIP call, and calls without rows are no work at all
 The records are packed as include/spanq.h lays them out; addresses are never followed."""
 import ctypes
 import math
+import struct
 
 import pytest
 
 spanq = pytest.importorskip("paper_2511_02749_amd")
 from paper_2511_02749_amd import row_ops as R  # noqa: E402
 
+QK_REC = struct.Struct("<10Q8q5i2fi")  # span_qk_norm
 P = 1 << 20  # an address: aligned, never read
 QK = dict(q=P, k=P, v=P, q_out=2 * P, k_out=2 * P, v_out=2 * P, q_gain=P, k_gain=P, rows=0, positions=0,
           q_stride=512, k_stride=128, v_stride=128, q_out_stride=512, k_out_stride=128, v_out_stride=128, n_rows=4,
@@ -53,7 +55,7 @@ def _refused(lib, entry, rec, args):
     dict(q_out=P, q_out_stride=520), dict(q_out=P, rows=P),
 ])
 def test_qk_norm_rope_refuses(lib, change):
-    _refused(lib, "span_qk_norm_rope", R._QK_REC, {**QK, **change})
+    _refused(lib, "span_qk_norm_rope", QK_REC, {**QK, **change})
 
 
 @pytest.mark.parametrize("change", [
@@ -91,8 +93,8 @@ def test_null_records_are_refused(lib):
 
 
 def test_calls_without_rows_are_no_work(lib):
-    assert _call(lib, "span_qk_norm_rope", R._QK_REC, {**QK, "n_rows": 0}) == 0
-    assert _call(lib, "span_qk_norm_rope", R._QK_REC, {**QK, **{n: 0 for n in ("q", "k", "v", "q_out", "k_out", "v_out")}}) == 0
+    assert _call(lib, "span_qk_norm_rope", QK_REC, {**QK, "n_rows": 0}) == 0
+    assert _call(lib, "span_qk_norm_rope", QK_REC, {**QK, **{n: 0 for n in ("q", "k", "v", "q_out", "k_out", "v_out")}}) == 0
     assert _call(lib, "span_adapter_apply", R._ADAPTER_REC, {**ADAPT, "n_rows": 0, "x": 0}) == 0
     assert _call(lib, "span_verify_drafts", R._VERIFY_REC, {**VERIFY, "n_requests": 0, "target": 0}) == 0
 
@@ -140,3 +142,21 @@ def test_tensors_on_the_host_are_refused():
         spanq.qk_norm_rope(None, None, None, None, None, 1e-5, None, None, None)
     with pytest.raises(spanq.SpanError):
         spanq.verify_drafts(torch.zeros(2, 9), None, None, torch.zeros(2), None, i, i[:, None])
+
+
+def test_what_is_no_tensor_on_a_gpu_is_refused_before_anything_else(lib):
+    torch = pytest.importorskip("torch")
+    x, i = torch.zeros(2, 64, dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32)
+    h, u = torch.zeros(2, 3, 64), torch.zeros(2)
+    a, b = torch.zeros(1, 1, 8, 64, dtype=torch.bfloat16), torch.zeros(1, 64, 8, dtype=torch.bfloat16)
+    for call in (lambda: spanq.qk_norm_rope(h, None, None, None, None, 1e-5, h, None, None),
+                 lambda: spanq.qk_norm_rope(None, None, None, None, None, 1e-5, None, None, None),
+                 lambda: spanq.qk_norm_rope(h.to_sparse(), None, None, None, None, 1e-5, h, None, None),
+                 lambda: spanq.qk_norm_rope([1.0], None, None, None, None, 1e-5, [1.0], None, None),
+                 lambda: spanq.adapter_apply(x, x, i, a, b, None, x), lambda: spanq.adapter_apply(None, x, i, a, b, None, x),
+                 lambda: spanq.adapter_apply(x, None, i, a, b, None, None),
+                 lambda: spanq.verify_drafts(u[None], None, None, u, None, i, i[:, None]),
+                 lambda: spanq.verify_drafts(u[None], None, None, u, None, i, None)):
+        with pytest.raises(spanq.SpanError) as e:
+            call()
+        assert e.value.code == -1

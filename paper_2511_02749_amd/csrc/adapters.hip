@@ -43,6 +43,7 @@ constexpr int kFewRows = 256;  // at most, of the few-row form (few_rows)
 // rank 128, whose partials are many, 35.7 -> 42.9.
 constexpr int kFewSlices = 8;
 constexpr int kManySlices = 16;
+constexpr int kXcds = 8;
 // Work-groups to which the adapters of a tile are dealt (in shrink, 2048 rows in four segments: 16.0
 // us with one, 12.9 with four; with eight, which are mostly empty, 1000 rows 23.4 -> 25.4 in all).
 constexpr int kManyGroups = 4;
@@ -216,7 +217,14 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
   __shared__ int list[16 * C::kRows];  // rows of the call
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int col_groups = (s.h_cols / 16 + C::kCols - 1) / C::kCols;
-  const int slice = blockIdx.x / col_groups, ct0 = (blockIdx.x % col_groups) * C::kCols;
+  // Few rows: a work-group for each slice and column group of every row.  Many: units of a tile and a
+  // slice are dealt to the XCDs, a unit's column groups one after another, so that x is fetched once,
+  // and with eight or sixteen slices one XCD alone fetches a slice of A.  1387 rows, K 13224, 96 columns
+  // of H: 33 us with five slices as they come, 23 with eight.
+  const int unit = kFew ? blockIdx.x / col_groups : blockIdx.x / (kXcds * col_groups) * kXcds + blockIdx.x % kXcds;
+  const int slice = kFew ? unit : unit % s.slices;
+  const int ct0 = (kFew ? blockIdx.x : blockIdx.x / kXcds) % col_groups * C::kCols;
+  const int64_t tile = kFew ? 0 : unit / s.slices;
   const int n_ct = min(C::kCols, s.h_cols / 16 - ct0);
   const int sub = s.k_slice / C::kWaves;
   const int k0 = slice * s.k_slice + wave * sub;
@@ -305,7 +313,8 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
     const int n = few_group(s, blockIdx.y, &aid, list);
     if (n > 0 && aid >= 0) work(aid, (1ull << n) - 1, [&](int i) -> int64_t { return list[i]; });
   } else {
-    const int64_t row0 = static_cast<int64_t>(blockIdx.y) * (16 * C::kRows);
+    const int64_t row0 = tile * (16 * C::kRows);
+    if (row0 >= s.rows) return;
     const int64_t row = row0 + lane;
     const unsigned long long live = __ballot(row < s.rows);
     const int2 at = row < s.rows ? s.order[row] : int2{0, -1};
@@ -535,12 +544,13 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(
 }
 
 // Many rows: 64 columns a wave, a run of tiles of 16 rows one after another.  The next tile's
-// base and H are on their way while a tile is worked, and the weights of the first kKept
-// blocks of ranks stay in registers while the adapter stays.  2048 rows of 28672 columns, rank 32,
-// move 235 MB in 56 us, 4.2 TB/s.
+// base and H are on their way while a tile is worked, and the weights of all kKept blocks of
+// ranks stay in registers while the adapter stays (2048 rows of 6144 columns, rank 128: 91 us in all,
+// 121 with six of the blocks fetched for every tile).  2048 rows of 28672 columns, rank 32, move 235
+// MB in 56 us, 4.2 TB/s; were the weights asked for only once the rank is known, 6 us more.
 constexpr int kManyJ = 4;
 constexpr int kManyRun = 8;  // at most
-constexpr int kKept = 2;
+template <int kKept>
 __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(const Shape s) {
   constexpr int J = kManyJ;
   using O = Out<J, true>;
@@ -590,7 +600,8 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
 #pragma unroll
     for (int k = 0; k < kKept; ++k)
 #pragma unroll
-      for (int j = 0; j < J; ++j) wv[k][j] = O::weights(s, cols, aid, j, m, 16 * k + 8 * (g & 1), rank, true);
+      for (int j = 0; j < J; ++j)
+        wv[k][j] = O::weights(s, cols, aid, j, m, 16 * k + 8 * (g & 1), rank, true);
     if (rank < 16 * kKept) {
 #pragma unroll
       for (int k = 0; k < kKept; ++k)
@@ -598,25 +609,12 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
         for (int j = 0; j < J; ++j) wv[k][j] = first_of(wv[k][j], rank - 16 * k - 8 * (g & 1));
     }
   };
-  auto multiply = [&](const Ahead& a, int t, f32x4_t (&acc)[J]) {
+  auto multiply = [&](const Ahead& a, f32x4_t (&acc)[J]) {
 #pragma unroll
     for (int k = 0; k < kKept; ++k)
 #pragma unroll
       for (int j = 0; j < J && 16 * k < rank; ++j)
         acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(a.h[k]), as_frag(wv[k][j]), acc[j], 0, 0, 0);
-    for (int rb = kKept; 16 * rb < rank; ++rb) {
-      const uint4 h = load_h(16 * t + m, rb);
-      uint4 w[J];
-#pragma unroll
-      for (int j = 0; j < J; ++j) w[j] = O::weights(s, cols, kept, j, m, 16 * rb + 8 * (g & 1), rank, true);
-      if (16 * rb + 16 > rank) {
-#pragma unroll
-        for (int j = 0; j < J; ++j) w[j] = first_of(w[j], rank - 16 * rb - 8 * (g & 1));
-      }
-#pragma unroll
-      for (int j = 0; j < J; ++j)
-        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(h), as_frag(w[j]), acc[j], 0, 0, 0);
-    }
   };
   // The usual run, whole and of one adapter, in a loop without a condition on a load or
   // store: each would make the next wait for all of them, stores included.
@@ -632,7 +630,7 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
       now = ahead;
       fetch(t + 1, ahead);  // (of the last tile: the last row again)
       f32x4_t acc[J] = {};
-      multiply(now, t, acc);
+      multiply(now, acc);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         O::store(out, s.out_stride, cols, list[16 * t + 4 * g + i], m, O::add(now.base[i], acc, i, scale));
@@ -648,7 +646,7 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
       f32x4_t acc[J] = {};
       if (aid >= 0) {
         if (aid != kept) keep(aid);
-        multiply(now, t, acc);
+        multiply(now, acc);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -700,17 +698,19 @@ Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows, size_t* 
   for (int p = 0; p < c.n_parts; ++p) s.N += s.cols[p] = c.part_cols[p];
   s.rank_blocks = (s.R + 15) / 16;
   s.h_cols = 16 * s.n_parts * s.rank_blocks;
-  // K slices: enough work-groups for the chip
+  // K slices: enough work-groups for the chip, and for many rows a multiple of the XCDs' number where K
+  // allows it and partials are not too many (10000 rows: K 4096, 16 columns of H 88 us with eight, 102
+  // with one; K 2048, 128 columns 122 and 95)
   const bool few = rows <= few_rows(s);
   const int unit = 32 * (few ? FewShrink::kSteps * FewShrink::kWaves : ManyShrink::kSteps * ManyShrink::kWaves);
   const int64_t most = (s.K + unit - 1) / unit;
   const int64_t tiles = (rows + 16 * kManyTiles - 1) / (16 * kManyTiles) * h_groups<ManyShrink>(s);
-  const int64_t want = few ? kFewSlices : std::min<int64_t>(kManySlices, 256 / std::max<int64_t>(1, tiles));
+  const int64_t want = few ? kFewSlices : (tiles >= 256 ? 1 : tiles > 16 ? kXcds : kManySlices);
   const int64_t n = std::max<int64_t>(1, std::min(want, most));
   s.k_slice = static_cast<int>(((s.K + n - 1) / n + unit - 1) / unit * unit);
   s.slices = (s.K + s.k_slice - 1) / s.k_slice;
-  // runs as long as leave two work-groups for a CU
-  s.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kManyRun, (rows + 15) / 16 * col_blocks<kManyJ>(s) / 512)));
+  // runs as long as leave three work-groups for a CU
+  s.run = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(kManyRun, (rows + 15) / 16 * col_blocks<kManyJ>(s) / 768)));
   const bool tile = few || (s.run == 1 && s.N <= kNarrow && s.slices * s.rank_blocks <= kTilePartials);
   const int64_t plane = rows * s.h_cols, planes = tile || s.slices > 1 ? s.slices : 0;
   s.part = static_cast<float*>(c.workspace);
@@ -766,7 +766,7 @@ hipError_t launch_adapter_apply(const span_adapter_call& a, hipStream_t st) {
       adapter_order_kernel<<<1, kOrderThreads, 0, st>>>(s);
       e = hipGetLastError();
       if (e != hipSuccess) return e;
-      adapter_shrink_kernel<false, ManyShrink><<<dim3(s.slices * h_groups<ManyShrink>(s), tiles, kManyGroups), 64 * ManyShrink::kWaves, 0, st>>>(s);
+      adapter_shrink_kernel<false, ManyShrink><<<dim3((tiles * s.slices + kXcds - 1) / kXcds * kXcds * h_groups<ManyShrink>(s), 1, kManyGroups), 64 * ManyShrink::kWaves, 0, st>>>(s);
       e = hipGetLastError();
       if (e == hipSuccess && s.h && s.slices > 1) {
         adapter_finish_kernel<<<static_cast<unsigned>((s.rows * s.h_cols / 4 + 255) / 256), 256, 0, st>>>(s);
@@ -774,8 +774,13 @@ hipError_t launch_adapter_apply(const span_adapter_call& a, hipStream_t st) {
       }
       if (e != hipSuccess) return e;
       const unsigned runs = static_cast<unsigned>((s.rows + 16 * s.run - 1) / (16 * s.run));
-      if (s.h)
-        adapter_expand_many_kernel<<<dim3(col_blocks<kManyJ>(s), runs), 64 * kExpandWaves, 0, st>>>(s);
+      const dim3 grid(col_blocks<kManyJ>(s), runs);
+      if (s.h && s.rank_blocks <= 2)
+        adapter_expand_many_kernel<2><<<grid, 64 * kExpandWaves, 0, st>>>(s);
+      else if (s.h && s.rank_blocks <= 4)
+        adapter_expand_many_kernel<4><<<grid, 64 * kExpandWaves, 0, st>>>(s);
+      else if (s.h)
+        adapter_expand_many_kernel<8><<<grid, 64 * kExpandWaves, 0, st>>>(s);
       else
         adapter_expand_tile_kernel<false><<<dim3(col_blocks<kTileJ>(s), runs, kManyGroups), 64 * kExpandWaves, 0, st>>>(s);
     }

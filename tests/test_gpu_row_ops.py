@@ -221,7 +221,8 @@ def test_adapters_long_reductions_large_ranks_odd_widths(T, K, parts, R, S):
 
 
 @pytest.mark.parametrize("T,K,parts,R,S", [(200, 2048, (8200, 1000), 24, 5), (600, 4096, (264,), 128, 3), (1031, 520, (4104,), 40, 4),
-                                           (1100, 2048, (8, 8200), 16, 2), (2100, 264, (4096,), 8, 30)])
+                                           (1100, 2048, (8, 8200), 16, 2), (2100, 264, (4096,), 8, 30), (1500, 8200, (520, 4104, 8), 120, 7),
+                                           (700, 1032, (8200,), 56, 6)])
 def test_adapters_of_many_rows_and_columns(T, K, parts, R, S):
     """Wide products, large ranks and runs of tiles: mixed rows, and segments."""
     for ids in (None, [i * S // T - (i % 97 == 5) for i in range(T)]):

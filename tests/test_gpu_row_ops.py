@@ -684,6 +684,68 @@ def test_a_call_leaves_the_current_device_and_refuses_tensors_of_the_wrong_kind(
             spanq.verify_drafts(*args)
 
 
+def test_calls_of_two_threads_on_streams_of_their_own():
+    import threading
+    wrong, done = [], []
+
+    def work(seed):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            parts, T, V = (264, 24), (40, 300)[seed], 5000
+            case = _adapt_case(T, 520, parts, 24, 5, seed=seed)
+            d = [t.cuda(non_blocking=False) for t in case]
+            lg = torch.randn(6, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+            u = torch.rand(6, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed))
+            first = None
+            for _ in range(40):
+                out = torch.empty_like(d[1])
+                acc, tok = torch.empty(6, dtype=torch.int32, device="cuda"), torch.empty(6, 1, dtype=torch.int32, device="cuda")
+                spanq.adapter_apply(d[0], d[1], d[2], d[3], d[4], d[5], out, parts=parts, ranks=d[6])
+                spanq.verify_drafts(lg, None, None, u, None, acc, tok)
+                if first is None:
+                    first = (out, tok)
+                elif not (torch.equal(out, first[0]) and torch.equal(tok, first[1])):
+                    wrong.append(seed)
+            stream.synchronize()
+            ref, bound = _adapt_exact(*case, parts)
+            if not bool(((first[0].cpu().double() - ref).abs() <= bound).all()):
+                wrong.append(seed)
+            done.append(seed)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong and sorted(done) == [0, 1]
+
+
+def test_captured_calls_take_their_workspaces_from_the_graph():
+    """Without a workspace of the caller's: calls one after another in one graph, between them other memory."""
+    T, V, parts = 300, 3000, (72,)
+    case = _adapt_case(T, 136, parts, 16, 3, seed=1)
+    d = [t.cuda() for t in case]
+    lg, u = torch.randn(20, V, device="cuda"), torch.rand(20, device="cuda")
+    want, out, out2 = torch.empty_like(d[1]), torch.empty_like(d[1]), torch.empty_like(d[1])
+    acc, tok, tok2 = (torch.empty(20, *s, dtype=torch.int32, device="cuda") for s in ((), (1,), (1,)))
+    spanq.adapter_apply(d[0], d[1], d[2], d[3], d[4], d[5], want, ranks=d[6])
+    spanq.verify_drafts(lg, None, None, u, None, acc, tok2)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        spanq.adapter_apply(d[0], d[1], d[2], d[3], d[4], d[5], out, ranks=d[6])
+        mid = torch.full((T * 80,), float("nan"), device="cuda") * 2
+        spanq.verify_drafts(lg, None, None, u, None, acc, tok)
+        spanq.adapter_apply(d[0], d[1], d[2], d[3], d[4], d[5], out2, ranks=d[6])
+    for _ in range(3):
+        out.zero_()
+        out2.zero_()
+        tok.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(out2, want) and torch.equal(tok, tok2) and bool(torch.isnan(mid).all())
+
+
 # ------------------------------------------------------------------------ the largest sizes
 
 def _far(rows, width, stride, dtype):

@@ -664,15 +664,15 @@ unsigned h_groups(const Shape& s) {
 // Rows up to which the few-row form serves.  It reads B again for each 16 rows of an adapter,
 // the many-row form orders the rows first and gains by long runs.  Captured calls of K 4096, few /
 // many in us, 1 adapter and 32 mixed ones:
-//   N 4096, rank 16:   130 rows 15.0 / 14.4, 10.0 / 30.7   256 rows 20.2 / 14.6, 12.8 / 21.1
-//   N 28672, rank 32:   96 rows 25.7 / 19.1, 39.7 / 55.8   192 rows 42.7 / 22.1, 54.1 / 46.5
+//   N 4096, rank 16:   130 rows 15.0 / 13.2, 10.0 / 27.6   256 rows 20.2 / 13.3, 13.0 / 18.4
+//   N 28672, rank 32:   96 rows 25.5 / 19.0, 39.3 / 53.1   192 rows 42.7 / 25.0, 54.1 / 47.1
 constexpr int kNarrow = 8192;
 int few_rows(const Shape& s) { return s.N <= kNarrow ? kFewRows : kFewRows / 2; }
 
 // Many rows, but too few for runs: their expand adds the slices' partials up itself, up to so
 // many blocks of 16 ranks of them for a row, a launch less; every work-group across the columns does
 // it again.  Itself / by a launch, us:
-//   N 4096, rank 16:   257 rows 13.4 / 15.8, 384 rows of 32 mixed adapters 20.9 / 24.0
+//   N 4096, rank 16:   257 rows 13.7 / 16.2, 384 rows of 32 mixed adapters 20.8 / 23.6
 //   N 28672, rank 32:  130 rows 24.5 / 21.5, 32 mixed adapters 68.7 / 55.4
 constexpr int kTilePartials = 32;
 

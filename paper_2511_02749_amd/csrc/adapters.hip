@@ -16,9 +16,9 @@
 //
 // Matrix instructions 16x16x32, every operand 16 bytes of a row.  The second product's
 // columns are dealt to its tiles so that a lane's results of all tiles are columns that
-// follow one another, and base and out go as whole lines.  H enters it as two bf16 numbers, high and
-// low part (16 significant bits), side by side in the 32 deep reduction over the same 16
-// ranks, which costs nothing: the instruction is 32 deep and a block of ranks 16.
+// follow one another, and base and out go as whole lines.  H enters it as three bf16 numbers
+// that add up to it (24 significant bits): two of them side by side in the 32 deep reduction
+// over the same 16 ranks, the third in an instruction of its own.
 //
 // Bound: HBM (x, base and out for many rows, A and B for few); 2 R (K P + N) operations a row.
 // Decode steps are bound by the latency of their two launches and the loads in a row inside them.
@@ -38,6 +38,7 @@ using mfma::lo_bf16;
 using mfma::pack_bf16x2;
 
 constexpr int kTile = 16;      // rows of a group, ranks of a block
+constexpr int kParts = 3;      // bf16 numbers that hold a value of H: high, middle, low
 constexpr int kFewRows = 256;  // at most, of the few-row form (few_rows)
 // Work-groups over K at most.  Few rows, 16 for 8: 48 rows of K 14336 15.5 -> 14.7 us, but 200 rows of
 // rank 128, whose partials are many, 35.7 -> 42.9.
@@ -69,7 +70,7 @@ struct Shape {
   const float* scale;
   const int32_t* ranks;
   float* part;   // [slices][rows][h_cols] fp32
-  bf16_t* h;     // many rows: [rows][h_cols / 16][high 16, low 16]
+  bf16_t* h;     // many rows: [rows][h_cols / 16][kParts][16]
   int2* order;   // many rows: {row, its adapter or -1}, each adapter's rows together; H lies in this order
   int64_t rows, x_stride, base_stride, out_stride;
   int K, R, n_adapters, n_parts;
@@ -132,21 +133,39 @@ __device__ __forceinline__ void for_adapters(int id, unsigned long long live, F 
 
 __device__ __forceinline__ bf16x8_t as_frag(const uint4& v) { return __builtin_bit_cast(bf16x8_t, v); }
 
-// A float as the nearest bf16 and what that leaves of it (none of a value that is not finite),
-// for two of them packed.
-__device__ __forceinline__ void split2(float a, float b, uint32_t* high, uint32_t* low) {
-  *high = pack_bf16x2(a, b);
-  const float l0 = a - lo_bf16(*high), l1 = b - hi_bf16(*high);
-  *low = pack_bf16x2(isfinite(l0) ? l0 : 0.f, isfinite(l1) ? l1 : 0.f);
+// The upper halves of two words, packed.
+__device__ __forceinline__ uint32_t upper(uint32_t a, uint32_t b) { return a >> 16 | (b & 0xffff0000u); }
+
+// Two floats as their parts, packed: the upper half of the float, of what that leaves, and of what
+// is then left, 8 significant bits each, so that no more than 24 remain to be rounded (infinities
+// and NaN are the first part's alone).
+__device__ __forceinline__ void split3(float a, float b, uint32_t* part) {
+  uint32_t u = __float_as_uint(a), v = __float_as_uint(b);
+  part[0] = upper(u, v);
+#pragma unroll
+  for (int i = 1; i < kParts; ++i) {
+    const float x = __uint_as_float(u), y = __uint_as_float(v);
+    u = __float_as_uint(isfinite(x) ? x - hi_bf16(u) : 0.f);
+    v = __float_as_uint(isfinite(y) ? y - hi_bf16(v) : 0.f);
+    part[i] = upper(u, v);
+  }
 }
 
-// Four sums of H as their high and low parts, ranks 4 q .. of a block at h.
+// Four sums of H as their parts, ranks 4 q .. of a block at h.
 __device__ __forceinline__ void store_split(bf16_t* h, int q, const float4& sum) {
-  uint2 high, low;
-  split2(sum.x, sum.y, &high.x, &low.x);
-  split2(sum.z, sum.w, &high.y, &low.y);
-  reinterpret_cast<uint2*>(h)[q] = high;
-  reinterpret_cast<uint2*>(h)[q + 4] = low;
+  uint32_t lo[kParts], hi[kParts];
+  split3(sum.x, sum.y, lo);
+  split3(sum.z, sum.w, hi);
+#pragma unroll
+  for (int i = 0; i < kParts; ++i) reinterpret_cast<uint2*>(h)[q + 4 * i] = uint2{lo[i], hi[i]};
+}
+
+// acc[j] + the product of 32 ranks' worth of H with the weights of tile j
+template <int J>
+__device__ __forceinline__ void multiply_h(const uint4& h, const uint4 (&w)[J], f32x4_t (&acc)[J]) {
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+    acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(h), as_frag(w[j]), acc[j], 0, 0, 0);
 }
 
 __device__ __forceinline__ float4 operator+(const float4& a, const float4& b) {
@@ -302,7 +321,7 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
       const int r = (ct0 + c) % s.rank_blocks * 16 + 4 * q;  // past the rank H is zero
       sum = float4{r < rank ? sum.x : 0.f, r + 1 < rank ? sum.y : 0.f, r + 2 < rank ? sum.z : 0.f, r + 3 < rank ? sum.w : 0.f};
       if (!kFew && s.h && s.slices == 1)
-        store_split(s.h + 2 * (to * s.h_cols + (ct0 + c) * 16), q, sum);
+        store_split(s.h + kParts * (to * s.h_cols + (ct0 + c) * 16), q, sum);
       else
         *reinterpret_cast<float4*>(s.part + (slice * s.rows + to) * s.h_cols + (ct0 + c) * 16 + 4 * q) = sum;
     }
@@ -330,7 +349,7 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
   }
 }
 
-// Many rows: the slices' partials of H added up, as high and low parts (2048 rows, 64 columns, 8
+// Many rows: the slices' partials of H added up, as their parts (2048 rows, 64 columns, 8
 // slices: 5.0 us).
 __global__ __launch_bounds__(256) void adapter_finish_kernel(const Shape s) {
   const int64_t plane = s.rows * s.h_cols / 4;  // in vectors of four
@@ -343,7 +362,7 @@ __global__ __launch_bounds__(256) void adapter_finish_kernel(const Shape s) {
   float4 sum = v[0];
 #pragma unroll
   for (int i = 1; i < kManySlices; ++i) sum = sum + v[i];
-  store_split(s.h + 32 * (e / 4), static_cast<int>(e & 3), sum);
+  store_split(s.h + 16 * kParts * (e / 4), static_cast<int>(e & 3), sum);
 }
 
 // Zeroes elements n .. 7 of eight bf16 values.
@@ -438,7 +457,7 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(
   constexpr int J = kTileJ;
   using O = Out<J, false>;
   __shared__ int list[kTile];
-  __shared__ uint2 hs[128 / 16][kTile][2][4];  // [block of ranks][row][high, low][four ranks]
+  __shared__ __align__(16) uint2 hs[128 / 16][kTile][kParts][4];  // [block of ranks][row][part][four ranks]
   const int lane = threadIdx.x & 63;
   const int m = lane & 15, g = lane >> 4;
   const Cols cols = cols_of<J>(s, blockIdx.x, wave_id());
@@ -525,7 +544,9 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(
     formed = true;
     f32x4_t acc[J] = {};
     for (int rb = 0; 16 * rb < rank; ++rb) {
-      const uint4 hv = *reinterpret_cast<const uint4*>(&hs[rb][min(m, count - 1)][g >> 1][2 * (g & 1)]);
+      // ranks 8 (g & 1) .. of the block: high (g < 2) or middle parts, then low ones or nothing
+      const uint4* h = reinterpret_cast<const uint4*>(hs[rb][min(m, count - 1)]) + g;
+      const uint4 hv = h[0], low = g < 2 ? h[4] : uint4{0u, 0u, 0u, 0u};
       if (16 * rb + 16 > rank) {
 #pragma unroll
         for (int j = 0; j < J; ++j) wv[j] = first_of(wv[j], rank - 16 * rb - 8 * (g & 1));
@@ -533,9 +554,8 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(
       uint4 next[J];
 #pragma unroll
       for (int j = 0; j < J; ++j) next[j] = O::weights(s, cols, id, j, m, 16 * (rb + 1) + 8 * (g & 1), 0, true);
-#pragma unroll
-      for (int j = 0; j < J; ++j)
-        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(hv), as_frag(wv[j]), acc[j], 0, 0, 0);
+      multiply_h(hv, wv, acc);
+      multiply_h(low, wv, acc);
 #pragma unroll
       for (int j = 0; j < J; ++j) wv[j] = next[j];
     }
@@ -543,50 +563,68 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(
   }
 }
 
-// Many rows: 64 columns a wave, a run of tiles of 16 rows one after another.  The next tile's
-// base and H are on their way while a tile is worked, and the weights of all kKept blocks of
-// ranks stay in registers while the adapter stays (2048 rows of 6144 columns, rank 128: 91 us in all,
-// 121 with six of the blocks fetched for every tile).  2048 rows of 28672 columns, rank 32, move 235
-// MB in 56 us, 4.2 TB/s; were the weights asked for only once the rank is known, 6 us more.
+// Many rows: 64 columns a wave, a run of tiles of 16 rows one after another.  The run's H lies in
+// LDS, which the four waves read instead of each fetching it (three parts of H from memory: 2048 rows of 28672
+// columns 64 us, from LDS 57); the next tile's base is on its way while a tile is worked, and the weights of
+// all kKept blocks of ranks stay in registers while the adapter stays (2048 rows of 6144 columns, rank 128: 67 us
+// in all).  2048 rows of 28672 columns, rank 32, move 235 MB in 57 us, 4.1 TB/s; were the
+// weights asked for only once the rank is known, 6 us more.  Short runs (kShortRun) have a form with room for no
+// more in LDS and registers: 300 rows of 8200 columns, rank 128, 37.6 us for 40.6.
 constexpr int kManyJ = 4;
 constexpr int kManyRun = 8;  // at most
-template <int kKept>
+constexpr int kShortRun = 2;
+template <int kKept, int kRun>
 __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(const Shape s) {
   constexpr int J = kManyJ;
   using O = Out<J, true>;
   const int lane = threadIdx.x & 63;
   const int m = lane & 15, g = lane >> 4;
-  __shared__ int list[16 * kManyRun];  // rows of the call
+  constexpr int kThreads = 64 * kExpandWaves;
+  constexpr int kVecs = 2 * kParts;            // of 16 bytes in a block of ranks
+  constexpr int kRowVecs = kVecs * kKept + 1;  // (16 rows' reads fall on different banks)
+  __shared__ int list[16 * kRun];  // rows of the call
+  __shared__ uint4 hs[16 * kRun * kRowVecs];
   const Cols cols = cols_of<J>(s, blockIdx.x, wave_id());
   const bool in_place = s.base == s.out && s.base_stride == s.out_stride;
   const bool has_col = cols.n0 + J * m < cols.width;
   const int64_t row0 = static_cast<int64_t>(blockIdx.y) * (16 * s.run);
   const int n_rows = static_cast<int>(min<int64_t>(16 * s.run, s.rows - row0));
-  int ids[(16 * kManyRun + 63) / 64];
+  int ids[(16 * kRun + 63) / 64], rows[(16 * kRun + 63) / 64];
 #pragma unroll
-  for (int i = 0; i < (16 * kManyRun + 63) / 64; ++i) {
+  for (int i = 0; i < (16 * kRun + 63) / 64; ++i) {
     const int2 at = 64 * i + lane < n_rows ? s.order[row0 + 64 * i + lane] : int2{0, -1};
+    rows[i] = at.x;
     ids[i] = at.y;
-    if (wave_id() == 0 && 64 * i + lane < n_rows) list[64 * i + lane] = at.x;
+  }
+  // The run's H, which all waves read, in LDS; asked for together with the rows.  Rows past the last and
+  // blocks past the last hold some finite part: no result of theirs is used, or their weights are zero.
+  const uint4* h0 = reinterpret_cast<const uint4*>(s.h + kParts * (row0 * s.h_cols + cols.part * s.rank_blocks * 16));
+  constexpr int kAll = kVecs * kKept * 16 * kRun, kEach = (kAll + kThreads - 1) / kThreads;
+  uint4 hv[kEach];
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const int e = u * kThreads + threadIdx.x, r = min(e / (kVecs * kKept), n_rows - 1);
+    const int v = min(e % (kVecs * kKept), kVecs * s.rank_blocks - 1);
+    hv[u] = h0[static_cast<uint32_t>(r * (kVecs * s.h_cols / 16) + v)];
+  }
+#pragma unroll
+  for (int i = 0; i < (16 * kRun + 63) / 64; ++i)
+    if (wave_id() == 0 && 64 * i + lane < n_rows) list[64 * i + lane] = rows[i];
+#pragma unroll
+  for (int u = 0; u < kEach; ++u) {
+    const int e = u * kThreads + threadIdx.x;
+    if (kAll % kThreads == 0 || e < kAll) hs[e / (kVecs * kKept) * kRowVecs + e % (kVecs * kKept)] = hv[u];
   }
   __syncthreads();
   if (cols.n0 >= cols.width) return;
-  const char* h0 = reinterpret_cast<const char*>(s.h + 2 * (row0 * s.h_cols + cols.part * s.rank_blocks * 16));
-  // Of H, 16 bytes: ranks 8 (g & 1) .. of block rb, the high (g < 2) or low parts.  Rows past
-  // the last are read as the last, other adapters' rows as they are: no result of theirs is used.
-  auto load_h = [&](int r, int rb) {
-    const uint32_t at = 4 * min(r, n_rows - 1) * s.h_cols + 64 * min(rb, s.rank_blocks - 1) + 16 * g;
-    return *reinterpret_cast<const uint4*>(h0 + at);
-  };
+  // vector `at` of block rb of row r of H
+  auto load_h = [&](int r, int rb, int at) { return hs[r * kRowVecs + kVecs * rb + at]; };
   const bf16_t* base = s.base + cols.col0;
   bf16_t* out = s.out + cols.col0;
   struct Ahead {
     typename O::Vec base[4];
-    uint4 h[kKept];
   };
   auto fetch = [&](int t, Ahead& a) {
-#pragma unroll
-    for (int k = 0; k < kKept; ++k) a.h[k] = load_h(16 * t + m, k);
 #pragma unroll
     for (int i = 0; i < 4; ++i) a.base[i] = O::base(base, s.base_stride, cols, list[min(16 * t + 4 * g + i, n_rows - 1)], m);
   };
@@ -609,19 +647,26 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
         for (int j = 0; j < J; ++j) wv[k][j] = first_of(wv[k][j], rank - 16 * k - 8 * (g & 1));
     }
   };
-  auto multiply = [&](const Ahead& a, f32x4_t (&acc)[J]) {
+  // Of H, a lane's ranks 8 (g & 1) .. of a block: high (g < 2) or middle parts; of two blocks, the
+  // first's (g < 2) or the second's low parts.
+  auto multiply = [&](int t, f32x4_t (&acc)[J]) {
 #pragma unroll
-    for (int k = 0; k < kKept; ++k)
+    for (int k = 0; k < kKept; k += 2) {
+      if (16 * k >= rank) break;
+      uint4 w[J];  // (past the rank they are zero, and low parts are finite)
 #pragma unroll
-      for (int j = 0; j < J && 16 * k < rank; ++j)
-        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(a.h[k]), as_frag(wv[k][j]), acc[j], 0, 0, 0);
+      for (int j = 0; j < J; ++j) w[j] = g < 2 ? wv[k][j] : wv[k + 1][j];
+      multiply_h(load_h(16 * t + m, k + (g >> 1), 4 + (g & 1)), w, acc);
+      multiply_h(load_h(16 * t + m, k, g), wv[k], acc);
+      if (16 * k + 16 < rank) multiply_h(load_h(16 * t + m, k + 1, g), wv[k + 1], acc);
+    }
   };
   // The usual run, whole and of one adapter, in a loop without a condition on a load or
   // store: each would make the next wait for all of them, stores included.
   const int first = __builtin_amdgcn_readfirstlane(ids[0]);
   bool same = n_rows == 16 * s.run && cols.n0 + 16 * J <= cols.width && first >= 0;
 #pragma unroll
-  for (int i = 0; i < (16 * kManyRun + 63) / 64; ++i) same &= __ballot(64 * i + lane < n_rows && ids[i] != first) == 0;
+  for (int i = 0; i < (16 * kRun + 63) / 64; ++i) same &= __ballot(64 * i + lane < n_rows && ids[i] != first) == 0;
   if (same) {
     Ahead now, ahead;
     fetch(0, ahead);
@@ -630,7 +675,7 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
       now = ahead;
       fetch(t + 1, ahead);  // (of the last tile: the last row again)
       f32x4_t acc[J] = {};
-      multiply(now, acc);
+      multiply(t, acc);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         O::store(out, s.out_stride, cols, list[16 * t + 4 * g + i], m, O::add(now.base[i], acc, i, scale));
@@ -646,7 +691,7 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
       f32x4_t acc[J] = {};
       if (aid >= 0) {
         if (aid != kept) keep(aid);
-        multiply(now, acc);
+        multiply(t, acc);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -654,6 +699,14 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
           O::store(out, s.out_stride, cols, list[16 * t + 4 * g + i], m, aid < 0 ? now.base[i] : O::add(now.base[i], acc, i, scale));
     });
   }
+}
+
+template <int kKept>
+void launch_expand_many(const Shape& s, const dim3& grid, hipStream_t st) {
+  if (s.run <= kShortRun)
+    adapter_expand_many_kernel<kKept, kShortRun><<<grid, 64 * kExpandWaves, 0, st>>>(s);
+  else
+    adapter_expand_many_kernel<kKept, kManyRun><<<grid, 64 * kExpandWaves, 0, st>>>(s);
 }
 
 template <class C>
@@ -715,8 +768,9 @@ Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows, size_t* 
   const int64_t plane = rows * s.h_cols, planes = tile || s.slices > 1 ? s.slices : 0;
   s.part = static_cast<float*>(c.workspace);
   s.h = tile ? nullptr : reinterpret_cast<bf16_t*>(s.part + planes * plane);
-  s.order = few ? nullptr : reinterpret_cast<int2*>(s.part + (planes + !tile) * plane);
-  *bytes = (planes + !tile) * plane * sizeof(float) + (few ? 0 : rows * sizeof(int2));
+  const int64_t sums = planes * plane * sizeof(float) + (tile ? 0 : kParts * plane * sizeof(bf16_t));
+  s.order = few ? nullptr : reinterpret_cast<int2*>(static_cast<char*>(c.workspace) + sums);
+  *bytes = sums + (few ? 0 : rows * sizeof(int2));
   return s;
 }
 
@@ -776,11 +830,11 @@ hipError_t launch_adapter_apply(const span_adapter_call& a, hipStream_t st) {
       const unsigned runs = static_cast<unsigned>((s.rows + 16 * s.run - 1) / (16 * s.run));
       const dim3 grid(col_blocks<kManyJ>(s), runs);
       if (s.h && s.rank_blocks <= 2)
-        adapter_expand_many_kernel<2><<<grid, 64 * kExpandWaves, 0, st>>>(s);
+        launch_expand_many<2>(s, grid, st);
       else if (s.h && s.rank_blocks <= 4)
-        adapter_expand_many_kernel<4><<<grid, 64 * kExpandWaves, 0, st>>>(s);
+        launch_expand_many<4>(s, grid, st);
       else if (s.h)
-        adapter_expand_many_kernel<8><<<grid, 64 * kExpandWaves, 0, st>>>(s);
+        launch_expand_many<8>(s, grid, st);
       else
         adapter_expand_tile_kernel<false><<<dim3(col_blocks<kTileJ>(s), runs, kManyGroups), 64 * kExpandWaves, 0, st>>>(s);
     }

@@ -55,7 +55,8 @@ struct Args {
   int chunks;
   int q0;          // first request of the launch
   Stat* target;    // [requests][drafts + 1][chunks]
-  Stat* draft;     // [requests][drafts][chunks]
+  Stat* draft;     // [requests][drafts][chunks]; without distributions, of each draft its own chunk alone:
+                   // what target row j holds there without drafted token j
   double* left;    // [requests][chunks]: sums of max(p - q, 0)
 };
 
@@ -201,6 +202,38 @@ __device__ __forceinline__ void load_chunk(const float* __restrict__ row, int ba
   }
 }
 
+// What a chunk's sum is in the row's scale; nothing where its largest weight would not be a normal
+// number there, so that a chunk with a sum has a token with a weight.
+__device__ __forceinline__ double in_row(const Stat& chunk, const Scale& row) {
+  if (row.hot) return chunk.max == row.only ? chunk.sum : 0.0;
+  const double octaves = rint(static_cast<double>(chunk.max) * row.c) - row.k;
+  const double sum = octaves >= -1021.0 ? chunk.sum : 0.0;
+  return ldexp(sum, static_cast<int>(fmax(octaves, -1021.0)));
+}
+
+// Largest of a wave's logits, -inf if none is a number.
+template <int kPer>
+__device__ __forceinline__ float chunk_max(const float (&x)[kPer]) {
+  float best = x[0];
+#pragma unroll
+  for (int u = 1; u < kPer; ++u) best = fmaxf(best, x[u]);
+  best = wave_max(best);
+  return best > -INFINITY ? best : -INFINITY;
+}
+// Sum of a wave's weights.
+template <int kPer>
+__device__ __forceinline__ double chunk_sum(const float (&x)[kPer], const Scale& s) {
+  double sum = 0.0;
+  if (s.hot) {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) sum += x[u] == s.only ? 1.0 : 0.0;
+  } else {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) sum += weight_at(x[u], s);
+  }
+  return wave_sum(sum);
+}
+
 // ------------------------------------------------------------------ 1: chunks of every row
 template <int kChunk>
 __global__ __launch_bounds__(kThreads) void verify_stats_kernel(const Args a) {
@@ -217,13 +250,12 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(const Args a) {
   const float* row = draft ? c.draft_logits + (r.draft_row + j) * c.draft_stride
                            : c.target_logits + (r.target_row + j) * c.target_stride;
   const int base = chunk * kChunk;
+  int held = -1;  // drafted token j
+  if (!draft && !c.draft_logits && !r.greedy && j < r.n_drafts) held = c.drafts[static_cast<int64_t>(q) * k + j];
+  if (held >= c.vocab) held = -1;
   float x[kPer];
   load_chunk(row, base, lane, c.vocab, x);
-  float best = x[0];
-#pragma unroll
-  for (int u = 1; u < kPer; ++u) best = fmaxf(best, x[u]);
-  best = wave_max(best);
-  if (!(best > -INFINITY)) best = -INFINITY;  // a chunk of NaN
+  const float best = chunk_max(x);
   int arg = INT32_MAX;
   if (r.greedy) {
 #pragma unroll
@@ -231,28 +263,27 @@ __global__ __launch_bounds__(kThreads) void verify_stats_kernel(const Args a) {
       if (x[u] == best) arg = id_of(base, lane, u);  // a lane's ids rise with u
     arg = wave_min(arg);
   }
-  double sum = 0.0;
   const Scale s = scale_of(best, r.c);
-  if (s.hot) {
+  double sum;
+  if (held >= base && held < base + kChunk) {
+    // A refused draft without a distribution leaves the row without that token, which a difference
+    // of sums would not tell from a rounding: its chunk is added up without it, the token last.
+    const float token = row[held];
 #pragma unroll
-    for (int u = 0; u < kPer; ++u) sum += x[u] == s.only ? 1.0 : 0.0;
+    for (int u = 0; u < kPer; ++u)
+      if (id_of(base, lane, u) == held) x[u] = -INFINITY;
+    Stat rest{0.0, chunk_max(x), INT32_MAX};
+    rest.sum = chunk_sum(x, scale_of(rest.max, r.c));
+    sum = in_row(rest, s) + weight(token, s);
+    if (lane == 0) a.draft[(static_cast<int64_t>(q) * k + j) * a.chunks + chunk] = rest;
   } else {
-#pragma unroll
-    for (int u = 0; u < kPer; ++u) sum += weight_at(x[u], s);
+    sum = chunk_sum(x, s);
   }
-  sum = wave_sum(sum);
   if (lane == 0) {
     Stat* to = draft ? a.draft + (static_cast<int64_t>(q) * k + j) * a.chunks
                      : a.target + (static_cast<int64_t>(q) * (k + 1) + j) * a.chunks;
     to[chunk] = Stat{sum, best, arg};
   }
-}
-
-// What a chunk's sum is in the row's scale.
-__device__ __forceinline__ double in_row(const Stat& chunk, const Scale& row) {
-  if (row.hot) return chunk.max == row.only ? chunk.sum : 0.0;
-  const double octaves = rint(static_cast<double>(chunk.max) * row.c) - row.k;
-  return ldexp(chunk.sum, static_cast<int>(fmax(octaves, -3000.0)));
 }
 
 // A row's largest logit, its lowest id (greedy requests) and its sum of weights, by one wave;
@@ -278,7 +309,7 @@ __device__ __forceinline__ Stat whole_row(const Stat* st, int chunks, const Requ
 
 // What the work-groups of 2 and 3 need of a request's rows.
 struct Verdict {
-  Stat p[kMaxDrafts + 1], q[kMaxDrafts];
+  Stat p[kMaxDrafts + 1], q[kMaxDrafts];  // (q without distributions: what a draft's chunk holds without it)
   float x[kMaxDrafts];  // the drafted tokens' logits
   int d[kMaxDrafts], keep[kMaxDrafts];
 };
@@ -286,7 +317,8 @@ struct Verdict {
 // Acceptance of a request's drafts, by all waves of the work-group; returns the number
 // kept.  p and q of `v` hold the rows' sums afterwards, chunk[j][i] (if given) what chunk i < 64
 // adds to target row j's.
-template <int kNW>
+// kChunk: of the chunks, where v.q is to hold what they have without the drafts; 0: not asked for.
+template <int kNW, int kChunk>
 __device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Verdict& v,
                                       double (*chunk)[64] = nullptr) {
   const span_verify_call& c = a.c;
@@ -296,13 +328,20 @@ __device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Ve
   // the drafted tokens and their logits: asked for first, used last
   const int mine = static_cast<int>(threadIdx.x);
   int d = -1;
-  float x = 0.f, y = 0.f, u = 0.f;
+  float x = 0.f, y = 0.f, u = 0.f, rest_max = -INFINITY;
+  double rest = 0.0;
   if (mine < r.n_drafts) {
     d = c.drafts[static_cast<int64_t>(q) * k + mine];
     u = c.u_accept[static_cast<int64_t>(q) * k + mine];
     if (d >= 0 && d < c.vocab) {
       x = c.target_logits[(r.target_row + mine) * c.target_stride + d];
       if (dist) y = c.draft_logits[(r.draft_row + mine) * c.draft_stride + d];
+      if constexpr (kChunk > 0)
+        if (!dist && !r.greedy) {
+          const Stat& st = a.draft[(static_cast<int64_t>(q) * k + mine) * a.chunks + d / kChunk];
+          rest = st.sum;
+          rest_max = st.max;
+        }
     }
   }
   for (int e = wave; e < r.n_drafts + 1 + (dist ? r.n_drafts : 0); e += kNW) {
@@ -330,6 +369,8 @@ __device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Ve
     v.keep[j] = keep;
     v.d[j] = d;
     v.x[j] = x;
+    if constexpr (kChunk > 0)
+      if (!dist) v.q[j] = Stat{rest, rest_max, INT32_MAX};
   }
   __syncthreads();
   int n = 0;
@@ -387,7 +428,7 @@ __global__ __launch_bounds__(kThreads) void verify_left_kernel(const Args a) {
   const int lane = threadIdx.x & 63;
   const Request r = request_of(c, q);
   if (!r.valid || r.greedy || r.n_drafts == 0) return;
-  const int n = accept<kWaves>(a, q, r, v);
+  const int n = accept<kWaves, 0>(a, q, r, v);
   const int chunk = blockIdx.x * (kWaves) + (threadIdx.x >> 6);
   if (n == r.n_drafts || chunk >= a.chunks) return;  // after the last draft the chunks' own sums serve
   const Left l = left_of(a, q, r, v, n, false);
@@ -439,7 +480,7 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
     s_last = -1;
   }
   const float u_sample = c.u_sample[q];
-  const int n = accept<kPickWaves>(a, q, r, v, s_chunk);  // (its barriers also publish s_first and s_last)
+  const int n = accept<kPickWaves, kChunk>(a, q, r, v, s_chunk);  // (its barriers also publish s_first and s_last)
   int token = -1;
   if (!(v.p[n].sum > 0.0)) {
   } else if (r.greedy) {
@@ -456,9 +497,8 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
       auto chunk_sum = [&](int i) -> double {
         if (i >= a.chunks) return 0.0;
         if (l.y) return a.left[static_cast<int64_t>(q) * a.chunks + i];
-        double s = (i < 64 ? s_chunk[n][i] : in_row(st[i], l.p)) * l.ps;
-        if (l.one_hot >= 0 && l.one_hot / kChunk == i) s -= weight(v.x[n], l.p) * l.ps;
-        return s > 0.0 ? s : 0.0;
+        if (l.one_hot >= 0 && l.one_hot / kChunk == i) return in_row(v.q[n], l.p) * l.ps;
+        return (i < 64 ? s_chunk[n][i] : in_row(st[i], l.p)) * l.ps;
       };
       const double own = chunk_sum(lane);  // all of them up to 64 chunks
       double total = 0.0;

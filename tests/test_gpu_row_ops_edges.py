@@ -7,6 +7,7 @@ import numpy as np
 import pytest
 
 import paper_2511_02749_amd as spanq
+from tests.test_gpu_row_ops import _logits, _verify_and_check
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -52,3 +53,41 @@ def test_adapters_keep_every_bit_of_the_low_rank_sums(T, N, R):
     spanq.adapter_apply(x.to(bf).cuda(), torch.zeros_like(out), ids.to(torch.int32).cuda(), a.to(bf).cuda(), b.to(bf).cuda(),
                         None, out)
     assert torch.equal(out.cpu().float(), want), float((out.cpu().float() - want).abs().max())
+
+
+# ------------------------------------------------------------------------ verification
+
+@pytest.mark.parametrize("V,n", [(1500, 60), (3000, 60), (40000, 40), (128256, 20)])
+def test_a_refused_draft_that_stands_alone_in_its_chunk_leaves_nothing_there(V, n):
+    """Grammar masks that allow the draft and a token far from it: with a random number of 0 (and next to it)
+    the first chunk with any weight decides, and that of the refused draft has none."""
+    k = 2
+    target, _, drafts, ua, us, heat = _logits(n, k, V, V, False)
+    heat = heat.clamp(min=0.2) + 0.1
+    t, g = target.view(n, k + 1, V), _gen(V)
+    drafts = torch.randint(0, 400, (n, k), generator=g).to(torch.int32)  # in the first chunk, of 512 at least
+    other = torch.randint(V - 300, V, (n,), generator=g)
+    keep = t.clone()
+    t[:] = -float("inf")
+    for i in range(n):
+        for j in range(k):
+            t[i, j, drafts[i, j]] = keep[i, j, 0]
+        t[i, :, other[i]] = keep[i, :, 1]
+    ua[:] = 1 - 2.0 ** -24
+    us[:] = torch.tensor([0.0, 0.0, 1e-30, 2.0 ** -24] * (n // 4))
+    acc, tok, _ = _verify_and_check(target, None, drafts, None, ua, us, heat, None, None, k, f"alone in its chunk, V {V}")
+    assert (acc == 0).any() and np.array_equal(tok[np.arange(n), acc], other.numpy())
+
+
+def test_weights_too_small_for_a_number_are_passed_over():
+    """Chunks before the row's largest logits whose single weights are no number in 64 bits, though
+    their sum would be: with a random number of 0 the token is the first one that has a weight."""
+    n, V = 12, 6000
+    target = torch.full((n, V), -float("inf"))
+    first = torch.randint(4000, V, (n,), generator=_gen(1))
+    for i in range(n):
+        target[i, :3000] = -744.5 - 0.25 * i  # exp: below half of the smallest number from -745.14 on
+        target[i, first[i]:] = 0.0
+    us = torch.zeros(n)
+    _, tok, _ = _verify_and_check(target, None, None, None, None, us, None, None, None, 0, "weights that are no number")
+    assert np.array_equal(tok[3:, 0], first[3:].numpy())

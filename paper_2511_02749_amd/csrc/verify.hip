@@ -380,6 +380,14 @@ __device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Ve
 
 __device__ __forceinline__ double inverse(double s) { return s > 0.0 ? 1.0 / s : 0.0; }
 
+// max(p - q, 0) of two weights and the inverses of their rows' sums, each product rounded: contracted
+// to an fma the difference of equal ones would be a rounding, not 0, and where p = q nothing may be left.
+__device__ __forceinline__ double residue(double p, double ps, double q, double qs) {
+#pragma clang fp contract(off)
+  const double a = p * ps, b = q * qs;
+  return fmax(a - b, 0.0);
+}
+
 // What the row that decides a request leaves of a token: max(p - q, 0), or p.
 struct Left {
   const float* x;
@@ -388,9 +396,8 @@ struct Left {
   double ps, qs;  // 1 / sums
   int one_hot;    // the token taken out of p where the draft has no distribution, -1: none
   __device__ __forceinline__ double of(int i, float xi, float yi) const {
-    double w = weight(xi, p) * ps;
-    if (y) w = fmax(w - weight(yi, q) * qs, 0.0);
-    return i == one_hot ? 0.0 : w;
+    if (y) return residue(weight(xi, p), ps, weight(yi, q), qs);
+    return i == one_hot ? 0.0 : weight(xi, p) * ps;
   }
 };
 
@@ -442,8 +449,7 @@ __global__ __launch_bounds__(kThreads) void verify_left_kernel(const Args a) {
     for (int u = 0; u < kPer; ++u) sum += l.of(-2, x[u], y[u]);
   } else {
 #pragma unroll
-    for (int u = 0; u < kPer; ++u)
-      sum += fmax(weight_at(x[u], l.p) * l.ps - weight_at(y[u], l.q) * l.qs, 0.0);
+    for (int u = 0; u < kPer; ++u) sum += residue(weight_at(x[u], l.p), l.ps, weight_at(y[u], l.q), l.qs);
   }
   sum = wave_sum(sum);
   if (lane == 0) a.left[static_cast<int64_t>(q) * a.chunks + chunk] = sum;

@@ -91,3 +91,20 @@ def test_weights_too_small_for_a_number_are_passed_over():
     us = torch.zeros(n)
     _, tok, _ = _verify_and_check(target, None, None, None, None, us, None, None, None, 0, "weights that are no number")
     assert np.array_equal(tok[3:, 0], first[3:].numpy())
+
+
+@pytest.mark.parametrize("V", [700, 5003, 128256])
+def test_where_draft_and_target_agree_nothing_is_left_but_the_target(V):
+    """p = q in every token and a draft that no row has (outside the vocabulary, or without weight): max(p - q, 0) is
+    nothing, so the token comes from p itself."""
+    n, k = 24, 2
+    target, _, drafts, ua, us, heat = _logits(n, k, V, V, False)
+    heat = heat.clamp(min=0.2) + 0.1
+    t = target.view(n, k + 1, V)
+    drafts[::2] = torch.tensor([-1, V])
+    for i in range(1, n, 2):
+        t[i, :, 3::7] = -float("inf")
+        drafts[i] = 3
+    draft = t[:, :k].reshape(n * k, V).clone()
+    acc, _, _ = _verify_and_check(target, draft, drafts, None, ua * 0, us, heat, None, None, k, f"p = q, V {V}")
+    assert (acc == 0).all()

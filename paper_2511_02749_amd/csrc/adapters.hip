@@ -168,6 +168,35 @@ __device__ __forceinline__ void multiply_h(const uint4& h, const uint4 (&w)[J], 
     acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(h), as_frag(w[j]), acc[j], 0, 0, 0);
 }
 
+// A block of ranks of one row of H, as two operands.
+struct HRow {
+  uint4 first, low;
+};
+
+// Eight weights, infinite ones and NaN replaced by 0.  An infinite weight times H is what it is times H's
+// high part, which has H's sign and is 0 only where H is; a middle or low part may be 0 or of the
+// other sign and would make it NaN.
+__device__ __forceinline__ uint4 finite_of(const uint4& v) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
+    if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0xffffu;
+  }
+  return uint4{w[0], w[1], w[2], w[3]};
+}
+
+// Is any result of the tiles infinite or NaN?  Wave-uniform.
+template <int J>
+__device__ __forceinline__ bool any_wild(const f32x4_t (&acc)[J]) {
+  uint32_t most = 0;  // of the values' bits without their signs
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) most = max(most, __float_as_uint(fabsf(acc[j][i])));
+  return __ballot(most >= 0x7f800000u) != 0;
+}
+
 __device__ __forceinline__ float4 operator+(const float4& a, const float4& b) {
   return float4{a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w};
 }
@@ -423,6 +452,25 @@ struct Out {
       v[j] = pack_bf16x2(fmaf(scale, acc[2 * j][i], lo_bf16(base[j])), fmaf(scale, acc[2 * j + 1][i], hi_bf16(base[j])));
     return v;
   }
+  // The tiles' results once more, where one is infinite or NaN: only H's high parts meet infinite weights.
+  // (The weights are fetched again: kept for this, they would cost registers that every call has to give.)
+  template <class F>
+  static __device__ __forceinline__ void wild(const Shape& s, const Cols& c, int aid, int rank, int m, int g, F h_of,
+                                              f32x4_t (&acc)[J]) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) acc[j] = f32x4_t{};
+#pragma unroll 1
+    for (int rb = 0; 16 * rb < rank; ++rb) {
+      const HRow h = h_of(rb);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        const int r0 = 16 * rb + 8 * (g & 1);
+        const uint4 w = weights(s, c, aid, j, m, r0, rank, false), finite = finite_of(w);
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(h.low), as_frag(finite), acc[j], 0, 0, 0);
+        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(h.first), as_frag(g < 2 ? w : finite), acc[j], 0, 0, 0);
+      }
+    }
+  }
 };
 
 template <int J>
@@ -452,8 +500,10 @@ unsigned col_blocks(const Shape& s) {
 // kManyGroups work-groups, as in shrink.  64 rows of 64 adapters, 4096 columns, rank 16 (8.4 MB of
 // B): 7.5 us; 777 ordered rows of 2048 columns: 6.4.
 constexpr int kTileJ = 4;
+// (Few rows: five waves a SIMD, 96 registers. Left alone the compiler takes 120 for the sake of `wild`: 7.6 us for
+// 7.4 for one row.)
 template <bool kFew>
-__global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(const Shape s) {
+__global__ __launch_bounds__(64 * kExpandWaves, kFew ? 5 : 1) void adapter_expand_tile_kernel(const Shape s) {
   constexpr int J = kTileJ;
   using O = Out<J, false>;
   __shared__ int list[kTile];
@@ -542,11 +592,14 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(
     const float scale = s.scale ? s.scale[id] : 1.f;
     if (!formed) form();
     formed = true;
+    // of H, ranks 8 (g & 1) .. of a block: high (g < 2) or middle parts, then low ones or nothing
+    auto h_of = [&](int rb) {
+      const uint4* h = reinterpret_cast<const uint4*>(hs[rb][min(m, count - 1)]) + g;
+      return HRow{h[0], g < 2 ? h[4] : uint4{0u, 0u, 0u, 0u}};
+    };
     f32x4_t acc[J] = {};
     for (int rb = 0; 16 * rb < rank; ++rb) {
-      // ranks 8 (g & 1) .. of the block: high (g < 2) or middle parts, then low ones or nothing
-      const uint4* h = reinterpret_cast<const uint4*>(hs[rb][min(m, count - 1)]) + g;
-      const uint4 hv = h[0], low = g < 2 ? h[4] : uint4{0u, 0u, 0u, 0u};
+      const HRow h = h_of(rb);
       if (16 * rb + 16 > rank) {
 #pragma unroll
         for (int j = 0; j < J; ++j) wv[j] = first_of(wv[j], rank - 16 * rb - 8 * (g & 1));
@@ -554,11 +607,12 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(
       uint4 next[J];
 #pragma unroll
       for (int j = 0; j < J; ++j) next[j] = O::weights(s, cols, id, j, m, 16 * (rb + 1) + 8 * (g & 1), 0, true);
-      multiply_h(hv, wv, acc);
-      multiply_h(low, wv, acc);
+      multiply_h(h.first, wv, acc);
+      multiply_h(h.low, wv, acc);
 #pragma unroll
       for (int j = 0; j < J; ++j) wv[j] = next[j];
     }
+    if (__builtin_expect(any_wild(acc), 0)) O::wild(s, cols, id, rank, m, g, h_of, acc);
     put(mine, [&](int i) { return O::add(bv[i], acc, i, scale); });
   }
 }
@@ -659,6 +713,12 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
       multiply_h(load_h(16 * t + m, k + (g >> 1), 4 + (g & 1)), w, acc);
       multiply_h(load_h(16 * t + m, k, g), wv[k], acc);
       if (16 * k + 16 < rank) multiply_h(load_h(16 * t + m, k + 1, g), wv[k + 1], acc);
+    }
+    if (__builtin_expect(any_wild(acc), 0)) {
+      auto h_of = [&](int rb) {
+        return HRow{load_h(16 * t + m, rb, g), g < 2 ? load_h(16 * t + m, rb, 4 + g) : uint4{0u, 0u, 0u, 0u}};
+      };
+      O::wild(s, cols, kept, rank, m, g, h_of, acc);
     }
   };
   // The usual run, whole and of one adapter, in a loop without a condition on a load or

@@ -55,6 +55,42 @@ def test_adapters_keep_every_bit_of_the_low_rank_sums(T, N, R):
     assert torch.equal(out.cpu().float(), want), float((out.cpu().float() - want).abs().max())
 
 
+@pytest.mark.parametrize("T,N", FORMS)
+@pytest.mark.parametrize("R", [8, 40, 128])
+def test_adapters_with_infinite_weights(T, N, R):
+    """Infinite and NaN weights of B at ranks that count, with low-rank sums that a bf16 holds (nothing is left of
+    them), sums that it does not (a rest of either sign), and sums of 0: the formula's infinities and NaN, and
+    nothing else changes."""
+    g, S, K, bf = _gen(T * R), 3, 64, torch.bfloat16
+    x = torch.randint(-3, 4, (T, K), generator=g).float()
+    a = torch.randint(-2, 3, (S, 1, R, K), generator=g).float() * torch.tensor([1.0, 2.0 ** -9, 1.0])[:, None, None, None]
+    a[1, ..., :32] *= 2.0 ** 9  # sums of 12 bits and more
+    b = torch.randint(-2, 3, (S, N, R), generator=g).float()
+    ids = (torch.arange(T) * 7 // 5 % (S + 1) - 1).to(torch.int32)
+    base = torch.randint(-9, 10, (T, N), generator=g).float()
+    args = [t.cuda() for t in (x.to(bf), base.to(bf), ids, a.to(bf))]
+    plain, out = (torch.full((T, N), float("nan"), dtype=bf, device="cuda") for _ in range(2))
+    spanq.adapter_apply(*args, b.to(bf).cuda(), None, plain)
+    wild = torch.tensor([float("inf"), -float("inf"), float("nan")])
+    cols = torch.arange(1, N, 5)
+    for i in range(S - 1):  # (the last adapter has none)
+        b[i, cols, torch.randint(0, R, (len(cols),), generator=g)] = wild[torch.randint(0, 3, (len(cols),), generator=g)]
+        b[i, cols[::3], torch.randint(0, R, (len(cols[::3]),), generator=g)] = float("inf")
+    print(f"infinite weights T {T} N {N} R {R}", flush=True)
+    spanq.adapter_apply(*args, b.to(bf).cuda(), None, out)
+    h = torch.einsum("tk,srk->tsr", x.double(), a[:, 0].double())[torch.arange(T), ids.clamp(min=0).long()]
+    want = torch.zeros(T, N, dtype=torch.float64)
+    for i in range(S):
+        mine = (ids == i).nonzero()[:, 0]
+        terms = (h[mine][:, None] * b[i, cols].double()).sum(-1)  # infinities as the formula has them
+        want[mine[:, None], cols] = terms
+    out, plain = out.cpu(), plain.cpu()
+    assert bool((ids < 0).any()) and bool(torch.isposinf(want).any()) and bool(torch.isneginf(want).any()) and bool(want.isnan().any())
+    rest = want.isfinite()
+    assert torch.equal(out[rest], plain[rest])
+    assert torch.equal(out[~rest].double().nan_to_num(7.0, 8.0, 9.0), want[~rest].nan_to_num(7.0, 8.0, 9.0))
+
+
 # ------------------------------------------------------------------------ verification
 
 @pytest.mark.parametrize("V,n", [(1500, 60), (3000, 60), (40000, 40), (128256, 20)])

@@ -500,10 +500,8 @@ unsigned col_blocks(const Shape& s) {
 // kManyGroups work-groups, as in shrink.  64 rows of 64 adapters, 4096 columns, rank 16 (8.4 MB of
 // B): 7.5 us; 777 ordered rows of 2048 columns: 6.4.
 constexpr int kTileJ = 4;
-// (Few rows: five waves a SIMD, 96 registers. Left alone the compiler takes 120 for the sake of `wild`: 7.6 us for
-// 7.4 for one row.)
 template <bool kFew>
-__global__ __launch_bounds__(64 * kExpandWaves, kFew ? 5 : 1) void adapter_expand_tile_kernel(const Shape s) {
+__global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(const Shape s) {
   constexpr int J = kTileJ;
   using O = Out<J, false>;
   __shared__ int list[kTile];
@@ -614,6 +612,7 @@ __global__ __launch_bounds__(64 * kExpandWaves, kFew ? 5 : 1) void adapter_expan
     }
     if (__builtin_expect(any_wild(acc), 0)) O::wild(s, cols, id, rank, m, g, h_of, acc);
     put(mine, [&](int i) { return O::add(bv[i], acc, i, scale); });
+    if constexpr (kFew) return;
   }
 }
 

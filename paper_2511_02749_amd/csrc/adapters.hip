@@ -333,12 +333,12 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
       }
       multiply();
     }
-    // a lane holds ranks 4 g .. of row m of each tile
+    // A lane holds ranks 4 g .. of row m of each tile.  All tiles are stored, those past the last one too: no
+    // condition stands between a matrix instruction and the store of its result.
 #pragma unroll
     for (int t = 0; t < C::kRows; ++t)
 #pragma unroll
-      for (int c = 0; c < C::kCols; ++c)
-        if (c < n_ct) red[wave][c][16 * t + m][g] = __builtin_bit_cast(float4, acc[t][c]);
+      for (int c = 0; c < C::kCols; ++c) red[wave][c][16 * t + m][g] = __builtin_bit_cast(float4, acc[t][c]);
     __syncthreads();
     for (int e = threadIdx.x; e < n_ct * 64 * C::kRows; e += 64 * C::kWaves) {
       const int q = e & 3, row = (e >> 2) % (16 * C::kRows), c = e / (64 * C::kRows);

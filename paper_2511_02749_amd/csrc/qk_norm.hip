@@ -11,8 +11,9 @@
 // A lane holds 16 bytes of the head's first half and the 16 bytes d/2 further on, so both
 // members of a pair are in one lane, the sum of squares takes log2(lanes per head) lane
 // exchanges, and every access is a 16-byte vector.  A work-group takes one row: it puts its
-// cos and sin into LDS once (all heads share them), then walks the heads.  Angles are formed in 64 bits, in turns, and reduced to half a turn before the
-// 32-bit sine: at position 120000 a 32-bit product would be off by 0.004 radians.  Sums,
+// cos and sin into LDS once (all heads share them), then walks the heads.  Angles are formed in 64
+// bits, in turns, their cos and sin too: at position 120000 a 32-bit product would be off by 0.004
+// radians, and an angle rounded to 32 bits moves a small cos or sin by many of its last bits.  Sums,
 // norm and rotation are 32-bit; the only rounding to 16 bits is the result's.
 #include <hip/hip_runtime.h>
 
@@ -50,9 +51,9 @@ __global__ __launch_bounds__(kThreads) void qk_norm_kernel(const QkArgs g) {
       const double inv = exp2(-2.0 * i / D * g.log2_theta) * 0.15915494309189533577;  // turns per position
       double t = static_cast<double>(a.positions[row]) * inv;
       t -= rint(t);
-      float sn, cs;
-      sincospif(static_cast<float>(2.0 * t), &sn, &cs);
-      turn[i] = float2{cs, sn};
+      double sn, cs;
+      sincospi(2.0 * t, &sn, &cs);
+      turn[i] = float2{static_cast<float>(cs), static_cast<float>(sn)};
     }
     __syncthreads();
   }

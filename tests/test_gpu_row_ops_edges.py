@@ -144,3 +144,24 @@ def test_where_draft_and_target_agree_nothing_is_left_but_the_target(V):
     draft = t[:, :k].reshape(n * k, V).clone()
     acc, _, _ = _verify_and_check(target, draft, drafts, None, ua * 0, us, heat, None, None, k, f"p = q, V {V}")
     assert (acc == 0).all()
+
+
+# ------------------------------------------------------------------------ head norms
+
+@pytest.mark.parametrize("dim", [64, 128])
+@pytest.mark.parametrize("theta", [1e4, 5e5])
+def test_rotations_by_the_angle_and_not_by_a_float_next_to_it(dim, theta):
+    """Pairs (1, 0): the rotated ones are cos and sin, off by a rounding of their own, however small they are.
+    (Both sides' angles: a position of 18 bits times an inverse within 2^-51 of itself.)"""
+    n, g = 3000, _gen(dim)
+    pos = torch.randint(-50, 1 << 18, (n,), generator=g).to(torch.int32)
+    x = torch.zeros(n, 2, dim)
+    x[..., :dim // 2] = 1.0
+    y = torch.empty_like(x, device="cuda")
+    spanq.qk_norm_rope(x.cuda(), None, None, None, None, 0.0, y, None, None, positions=pos.cuda(), rope_theta=theta)
+    t = pos.double()[:, None] * theta ** (-2.0 * torch.arange(dim // 2, dtype=torch.float64) / dim)
+    want = torch.cat([torch.cos(t), torch.sin(t)], -1)[:, None].expand(-1, 2, -1)
+    err = (y.cpu().double() - want).abs()
+    bound = 2.0 ** -24 * want.abs() + 2.0 ** (18 - 50)
+    print(f"dim {dim} theta {theta}: worst err/bound {(err / bound).max():.3g}", flush=True)
+    assert bool((err <= bound).all())

@@ -52,6 +52,12 @@ def lookup_drafts(tokens: Sequence[int], n: int, longest: int = 3) -> List[int]:
     return []
 
 
+def _check_weight(tokens):
+    """Raises for -1, which stands where the logits leave no token any weight."""
+    if any(t < 0 for t in tokens):
+        raise RuntimeError("a query's logits leave no token any weight")
+
+
 @dataclass
 class Engine:
     pool: object                       # paper_2511_02749_amd.Pool (device, bf16)
@@ -98,6 +104,7 @@ class Engine:
                     for o, t in zip(out, cur):
                         o.append(t)
             else:
+                _check_weight(cur)
                 fed, kept = self._decode_checked(plan, history, out, max_tokens)
             st = plan.stats()
             self.calls.append(CallStats(queries=len(queries), pages_hit=st["pages_hit"], tokens_hit=st["tokens_hit"],
@@ -133,8 +140,6 @@ class Engine:
             seen[-1][:len(h) + len(o)] = h + o
         while any(len(o) < max_tokens for o in out):
             open_ = [len(o) < max_tokens for o in out]
-            if any(o[-1] < 0 for o in out):
-                raise RuntimeError("a query's logits leave no token any weight")
             drafts = [lookup_drafts(s[:len(h) + len(o)], min(self.n_drafts, max_tokens - len(o) - 1)) if go else []
                       for s, h, o, go in zip(seen, history, out, open_)]
             got = self.model.decode_drafts(
@@ -142,6 +147,7 @@ class Engine:
                 u_accept=[self._rng.random(len(d), np.float32) for d in drafts],
                 u_sample=self._rng.random(n, np.float32), temperature=np.full(n, self.temperature, np.float32),
                 stream=self.stream)
+            _check_weight(t for g in got for t in g)
             fed += sum(len(d) for d in drafts)
             kept += sum(len(g) - 1 for g in got if g)
             for s, h, o, g in zip(seen, history, out, got):

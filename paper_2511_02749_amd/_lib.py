@@ -632,6 +632,9 @@ class Model:
             heat = np.zeros(max(1, n), np.float32)
             us = np.zeros(max(1, n), np.float32)
             if temperature is not None:
+                for what, x in (("temperature", temperature), ("u_sample", u_sample), ("u_accept", u_accept)):
+                    if x is not None and not (what == "temperature" and np.ndim(x) == 0) and len(x) != n:
+                        raise SpanError(SPAN_EINVAL, f"decode_drafts: {what} needs an entry for each query")
                 heat[:n] = temperature
                 us[:n] = 0.0 if u_sample is None else u_sample
                 if u_sample is None and np.any(heat > 0):

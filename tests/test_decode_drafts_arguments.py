@@ -18,7 +18,8 @@ def _model(monkeypatch):
 
     class Lib:
         def span_model_decode_drafts(self, *args):
-            calls.append(args)
+            sampling = args[6]._obj
+            calls.append(([sampling.u_accept[i] for i in range(6)], [sampling.u_sample[i] for i in range(3)]))
             return 0
 
     monkeypatch.setattr(_lib, "load", lambda: Lib())
@@ -47,6 +48,5 @@ def test_an_entry_for_each_query_goes_to_the_library(monkeypatch):
     model, calls = _model(monkeypatch)
     for change in ({}, dict(temperature=0.7), dict(u_accept=[[0.5, 0.9], [0.1], [0.5, 0.5]])):
         assert model.decode_drafts(_Plan(), **{**GOOD, **change}) == [[], [], []]
-    sampling = calls[0][6]._obj
-    assert [sampling.u_accept[i] for i in range(6)] == [0.5, 0.0, 0.0, 0.0, 0.5, 0.5]
-    assert np.allclose([sampling.u_sample[i] for i in range(3)], [0.1, 0.2, 0.3]) and len(calls) == 3
+    accept, sample = calls[0]
+    assert accept == [0.5, 0.0, 0.0, 0.0, 0.5, 0.5] and np.allclose(sample, [0.1, 0.2, 0.3]) and len(calls) == 3

@@ -328,8 +328,10 @@ int span_plan_destroy(span_plan_t* plan);
  * Call after the plan's span_prefill_fragments / span_cross_attend calls for
  * every layer: once a step is planned those two return SPAN_ESTATE.
  * SPAN_ENOMEM (plan and pool unchanged) if the pages do not fit; SPAN_ESTATE after
- * commit; SPAN_EINVAL for plans of span_plan_static (a step allocates).  Host-only
- * pools plan the step (pages, positions) without device work. */
+ * commit; SPAN_EINVAL for plans of span_plan_static (a step allocates).  A step that
+ * fails after that (a call of the runtime, memory) appends nothing either: segments and
+ * pages are as before, but for cached pages that it evicted, and no step is planned.
+ * Host-only pools plan the step (pages, positions) without device work. */
 int span_plan_decode(span_plan_t* plan, const int32_t* n_new, const int64_t* rows, void* stream);
 
 /* The last decode step for one layer: write the new tokens' keys (rotated at their

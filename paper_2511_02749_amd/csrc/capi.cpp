@@ -848,38 +848,22 @@ static int decode_drain(span_plan_t* pl, hipStream_t s, const char* who) {
   return SPAN_OK;
 }
 
-int span_plan_decode(span_plan_t* pl, const int32_t* n_new, const int64_t* rows, void* stream) {
-  if (!pl) return fail(SPAN_EINVAL, "span_plan_decode: null plan");
-  if (pl->committed) return fail(SPAN_ESTATE, "span_plan_decode: plan already committed");
-  if (pl->in_scratch) return fail(SPAN_EINVAL, "span_plan_decode: decode steps allocate; not for span_plan_static plans");
-  Plan& P = pl->plan;
-  const size_t nq = P.query_spans.size();
-  if (nq > 0 && (!n_new || !rows)) return fail(SPAN_EINVAL, "span_plan_decode: null argument");
-  std::vector<int32_t> n(n_new, n_new + nq);
-  std::vector<int64_t> r(rows, rows + nq);
+// The planned step's work lists on the device, and scratch for its partials.
+static int upload_step(span_plan_t* pl, hipStream_t s) {
   span_pool* pool = pl->pool;
-  Tiling t = plan_tiling(pl);
-  t.materialize = (pool->cfg.flags & SPAN_FLAG_MATERIALIZE) != 0;
-  std::string msg;
-  int rc = pool->index->decode(&P, n, r, t, &msg);
-  if (rc) return fail(rc, "span_plan_decode: " + msg);
-  pl->decoding = true;
-  pl->rewound = false;
-  if (pool->cfg.device < 0) return SPAN_OK;
-  hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = hipSetDevice(pool->cfg.device);
   if (e != hipSuccess) return hip_fail(e, "span_plan_decode: hipSetDevice");
   // the previous step's device data are freed once their readers are done
-  rc = decode_drain(pl, s, "span_plan_decode");
+  int rc = decode_drain(pl, s, "span_plan_decode");
   if (rc) return rc;
   pool->blocks.give(pl->dec.block, s);
   pl->dec = span_plan_t::DecodeDev{};
-  rc = ensure_rope_table(pool, P.max_pos + 1, s);
+  rc = ensure_rope_table(pool, pl->plan.max_pos + 1, s);
   if (rc) return rc;
   // the host copy of the previous upload is reused once that upload is done
   if (pl->dec_copied && hipEventSynchronize(pl->dec_copied) != hipSuccess)
     return fail(SPAN_EHIP, "span_plan_decode: wait for the previous upload");
-  const Plan::DecodeStep& d = P.dec;
+  const Plan::DecodeStep& d = pl->plan.dec;
   auto& hb = pl->dec_host;
   hb.clear();
   const size_t o_w = put(hb, d.writes), o_kv = pl->mfma || pl->split ? 0 : put(hb, d.kv), o_kt = put(hb, d.kv_tiles), o_t = put(hb, d.tiles),
@@ -899,7 +883,12 @@ int span_plan_decode(span_plan_t* pl, const int32_t* n_new, const int64_t* rows,
     if (!pl->dec_ready) e = hipErrorOutOfMemory;
   }
   if (e == hipSuccess) e = hipEventRecord(pl->dec_ready, s);
-  if (e != hipSuccess) return hip_fail(e, "span_plan_decode: device metadata");
+  if (e != hipSuccess) {
+    (void)hipStreamSynchronize(s);  // the upload, if there is one, has left the host copy
+    pool->blocks.give(pl->dec.block, s);
+    pl->dec = span_plan_t::DecodeDev{};
+    return hip_fail(e, "span_plan_decode: device metadata");
+  }
   pl->dec_stream = s;
   pl->dec.writes = reinterpret_cast<const SlotWrite*>(pl->dec.meta + o_w);
   pl->dec.kv = reinterpret_cast<const KvPage*>(pl->dec.meta + o_kv);
@@ -908,6 +897,43 @@ int span_plan_decode(span_plan_t* pl, const int32_t* n_new, const int64_t* rows,
   pl->dec.cb = reinterpret_cast<const CombineTile*>(pl->dec.meta + o_cb);
   pl->dec.rope = pool->rope_tab;
   return SPAN_OK;
+}
+
+int span_plan_decode(span_plan_t* pl, const int32_t* n_new, const int64_t* rows, void* stream) {
+  if (!pl) return fail(SPAN_EINVAL, "span_plan_decode: null plan");
+  if (pl->committed) return fail(SPAN_ESTATE, "span_plan_decode: plan already committed");
+  if (pl->in_scratch) return fail(SPAN_EINVAL, "span_plan_decode: decode steps allocate; not for span_plan_static plans");
+  Plan& P = pl->plan;
+  const size_t nq = P.query_spans.size();
+  if (nq > 0 && (!n_new || !rows)) return fail(SPAN_EINVAL, "span_plan_decode: null argument");
+  try {
+    const std::vector<int32_t> n(n_new, n_new + nq);
+    const std::vector<int64_t> r(rows, rows + nq);
+    span_pool* pool = pl->pool;
+    Tiling t = plan_tiling(pl);
+    t.materialize = (pool->cfg.flags & SPAN_FLAG_MATERIALIZE) != 0;
+    const PoolIndex::BeforeDecode before = pool->index->before_decode(P);
+    const bool was_decoding = pl->decoding;
+    int rc = SPAN_OK;
+    try {
+      std::string msg;
+      rc = pool->index->decode(&P, n, r, t, &msg);
+      if (rc) return fail(rc, "span_plan_decode: " + msg);
+      pl->decoding = true;
+      pl->rewound = false;
+      if (pool->cfg.device >= 0) rc = upload_step(pl, static_cast<hipStream_t>(stream));
+    } catch (const std::exception& e) {
+      rc = fail(SPAN_ENOMEM, std::string("span_plan_decode: ") + e.what());
+    }
+    if (rc) {  // a step that fails appends nothing; the one before it is over all the same
+      pool->index->undo_decode(&P, before);
+      pl->decoding = was_decoding;
+      pl->rewound = true;
+    }
+    return rc;
+  } catch (const std::exception& e) {
+    return fail(SPAN_ENOMEM, std::string("span_plan_decode: ") + e.what());
+  }
 }
 
 int span_plan_rewind(span_plan_t* pl, const int32_t* n_drop) {

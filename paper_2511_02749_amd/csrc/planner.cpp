@@ -1022,27 +1022,50 @@ int PoolIndex::rewind(Plan* p, const std::vector<int32_t>& n_drop, std::string* 
       return SPAN_EINVAL;
     }
   p->dec = Plan::DecodeStep{};
+  for (size_t q = 0; q < nq; ++q) {
+    if (n_drop[q] == 0) continue;
+    p->decoded[q] -= n_drop[q];
+    cut_cross(p, q, p->spans[p->query_spans[q].back()].n_tok - n_drop[q]);
+  }
+  return SPAN_OK;
+}
+
+void PoolIndex::cut_cross(Plan* p, size_t q, int32_t n_tok) {
   // the last of `ids` that is `pid` (pages go from the end, where they were added)
   auto drop = [](std::vector<int32_t>& ids, int32_t pid) {
     const auto it = std::find(ids.rbegin(), ids.rend(), pid);
     if (it != ids.rend()) ids.erase(std::next(it).base());
   };
-  for (size_t q = 0; q < nq; ++q) {
-    if (n_drop[q] == 0) continue;
-    SpanPlan& cross = p->spans[p->query_spans[q].back()];
-    cross.n_tok -= n_drop[q];
-    p->decoded[q] -= n_drop[q];
-    const size_t keep = static_cast<size_t>((cross.n_tok + page_size_ - 1) / page_size_);
-    while (cross.pages.size() > keep) {
-      const int32_t pid = cross.pages.back();
-      cross.pages.pop_back();
-      drop(p->new_pages, pid);
-      drop(p->cross_pages, pid);
-      push_free(pid);
-    }
-    p->stale_tail[q] = cross.n_tok % page_size_ != 0;
+  SpanPlan& cross = p->spans[p->query_spans[q].back()];
+  cross.n_tok = n_tok;
+  const size_t keep = static_cast<size_t>((n_tok + page_size_ - 1) / page_size_);
+  while (cross.pages.size() > keep) {
+    const int32_t pid = cross.pages.back();
+    cross.pages.pop_back();
+    drop(p->new_pages, pid);
+    drop(p->cross_pages, pid);
+    push_free(pid);
   }
-  return SPAN_OK;
+  p->stale_tail[q] = n_tok % page_size_ != 0;
+}
+
+PoolIndex::BeforeDecode PoolIndex::before_decode(const Plan& p) const {
+  BeforeDecode b;
+  for (const auto& ids : p.query_spans) b.n_tok.push_back(p.spans[ids.back()].n_tok);
+  b.decoded = p.decoded;
+  b.steps = p.decode_steps;
+  b.tokens = p.decode_tokens;
+  b.pages = p.decode_pages;
+  return b;
+}
+
+void PoolIndex::undo_decode(Plan* p, const BeforeDecode& before) {
+  p->dec = Plan::DecodeStep{};
+  for (size_t q = 0; q < p->stale_tail.size(); ++q) cut_cross(p, q, before.n_tok[q]);
+  p->decoded = before.decoded;
+  p->decode_steps = before.steps;
+  p->decode_tokens = before.tokens;
+  p->decode_pages = before.pages;
 }
 
 void PoolIndex::commit(Plan* p) {

@@ -175,9 +175,20 @@ class PoolIndex {
   // work lists in p->dec.  Returns 0, -2 (pool full; plan and pool unchanged) or -1.
   int decode(Plan* p, const std::vector<int32_t>& n_new, const std::vector<int64_t>& rows, const Tiling& tiling,
              std::string* msg);
+  // What undo_decode needs to take a step back, asked for before it.
+  struct BeforeDecode {
+    std::vector<int32_t> n_tok, decoded;  // per query
+    int64_t steps = 0, tokens = 0, pages = 0;
+  };
+  BeforeDecode before_decode(const Plan& p) const;
+  // The segments and totals of before a step that was planned, or planned in part (cached pages that
+  // it evicted stay so).
+  void undo_decode(Plan* p, const BeforeDecode& before);
   // Take back the last n_drop[q] decoded tokens of each query's cross segment and free
   // the pages that held nothing else.  Returns 0 or -1 (nothing changed).
   int rewind(Plan* p, const std::vector<int32_t>& n_drop, std::string* msg);
+  // Query q's cross segment with its first n_tok tokens alone, other pages freed.
+  void cut_cross(Plan* p, size_t q, int32_t n_tok);
   void commit(Plan* p);
   void release(Plan* p);  // destroy without commit
   void reset();

@@ -78,6 +78,11 @@ int gpu_of(const char* name, const at::Tensor* t) {
 
 void* address(const at::Tensor& t) { return const_cast<void*>(t.const_data_ptr()); }
 
+// A tensor that a call has written: what autograd saved of it before is not what it holds now.
+void written(const at::Tensor* t) {
+  if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 struct Rows {
   void* at;
   int64_t stride;
@@ -244,6 +249,7 @@ PyObject* qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     c.rope_theta = static_cast<float>(number(a[11]));
     void* stream = stream_of(a[12], gpu);
     launch([&] { return bound.qk_norm_rope(&c, stream); });
+    for (const at::Tensor* t : out) written(t);
   });
 }
 
@@ -315,6 +321,7 @@ PyObject* adapter_apply(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     c.workspace_bytes = ws.bytes;
     void* stream = stream_of(a[10], gpu);
     launch([&] { return bound.adapter_apply(&c, stream); });
+    written(&out);
   });
 }
 
@@ -365,6 +372,7 @@ PyObject* verify_drafts(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     c.workspace_bytes = ws.bytes;
     void* stream = stream_of(a[13], gpu);
     launch([&] { return bound.verify_drafts(&c, stream); });
+    for (const int i : {5, 6, 11}) written(tensor("output", a[i]));
   });
 }
 

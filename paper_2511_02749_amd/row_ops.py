@@ -3,6 +3,8 @@ span_verify_drafts).  Argument marshalling only, most of it native (binding/rowo
 shapes and devices are checked there, sizes, strides and alignment by the library.
 
 Tensors lie on one GPU; a call is enqueued on `stream`, by default that GPU's current one.
+Outputs are written in place, as by torch's own in-place calls, but carry no history: the operators have no
+gradients, and none flow through them to inputs that require them.
 A workspace that is not given comes from torch's allocator, on the call's stream, and goes
 back to it when the call has been enqueued, as torch's own temporaries do.
 """

@@ -165,3 +165,28 @@ def test_rotations_by_the_angle_and_not_by_a_float_next_to_it(dim, theta):
     bound = 2.0 ** -24 * want.abs() + 2.0 ** (18 - 50)
     print(f"dim {dim} theta {theta}: worst err/bound {(err / bound).max():.3g}", flush=True)
     assert bool((err <= bound).all())
+
+
+# ------------------------------------------------------------------------ tensors
+
+def test_autograd_sees_that_outputs_were_written():
+    """A tensor that a graph saved and an operator wrote afterwards is refused by the backward pass, as after
+    torch's in-place calls; outputs have no history, also of inputs that require gradients."""
+    bf = torch.bfloat16
+    x, a, b = (torch.zeros(s, dtype=bf, device="cuda") for s in ((2, 64), (1, 1, 8, 64), (1, 64, 8)))
+    ids, h = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.ones(2, 1, 64, device="cuda")
+    lg, u = torch.zeros(2, 9, device="cuda"), torch.zeros(2, device="cuda")
+    acc, tok, lp = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.zeros(2, 1, dtype=torch.int32, device="cuda"), torch.zeros(2, 1, device="cuda")
+    out, qo = torch.ones_like(x), torch.ones_like(h)
+    for call, written in ((lambda: spanq.adapter_apply(x.requires_grad_(), x, ids, a, b, None, out), [out]),
+                          (lambda: spanq.qk_norm_rope(h.requires_grad_(), None, None, None, None, 1e-5, qo, None, None), [qo]),
+                          (lambda: spanq.verify_drafts(lg, None, None, u, None, acc, tok, logprobs=lp), [lp, acc, tok])):
+        w = torch.ones_like(written[0]).requires_grad_()
+        y = (w * written[0]).sum()
+        before = [t._version for t in written]
+        call()
+        assert all(t._version == v + 1 and not t.requires_grad for t, v in zip(written, before))
+        with pytest.raises(RuntimeError, match="inplace"):
+            y.backward()
+    with torch.inference_mode():
+        spanq.adapter_apply(x, x, ids, a, b, None, torch.empty_like(x))

@@ -585,6 +585,8 @@ class Model:
         """Head norms of the layers' queries and keys (span_model_set_qk_norm): a gain [head_dim] for
         each layer (None: not normed), or None for none."""
         L, d, device = self.cfg.num_layers, self.cfg.head_dim, self.pool.cfg.device
+        # (tuples: the tensors taken here are the ones kept, whatever becomes of the caller's lists)
+        q_norm, k_norm = (None if t is None else tuple(t) for t in (q_norm, k_norm))
         _check(load().span_model_set_qk_norm(self._h, _table("q_norm", q_norm, L, d, device),
                                              _table("k_norm", k_norm, L, d, device)))
         self._keep_norms = (q_norm, k_norm)
@@ -595,6 +597,7 @@ class Model:
         down is None or a pair (a, b) of per-layer sequences of device tensors (an entry may be None),
         a [n, parts, rank, in] and b [n, out, rank].  Without arguments: none."""
         c, device = self.cfg, self.pool.cfg.device
+        qkv, o, gate_up, down = (p and tuple(None if t is None else tuple(t) for t in p) for p in (qkv, o, gate_up, down))
         heads = c.num_q_heads * c.head_dim
         cfg = ModelAdapters(n_adapters=n_adapters, max_rank=max_rank,
                             scale=_weight("scale", scale, "float32", n_adapters, device),

@@ -63,7 +63,7 @@ extern "C" {
 
 #define SPAN_OK 0
 #define SPAN_EINVAL (-1)  /* bad argument or unsupported shape */
-#define SPAN_ENOMEM (-2)  /* pool exhausted: more pages needed than free or evictable */
+#define SPAN_ENOMEM (-2)  /* pool exhausted (more pages needed than free or evictable), or memory that could not be had */
 #define SPAN_EHIP (-3)    /* a HIP runtime call failed */
 #define SPAN_ESTATE (-4)  /* call-order violation (e.g. attention after commit) */
 

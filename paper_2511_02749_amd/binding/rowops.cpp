@@ -169,8 +169,8 @@ void launch(F f) {
   Py_END_ALLOW_THREADS checked(rc);
 }
 
-PyObject* refuse(const char* who, const std::string& what) {
-  PyObject* e = PyObject_CallFunction(bound.error, "is", SPAN_EINVAL, (std::string(who) + ": " + what).c_str());
+PyObject* refuse(const char* who, const std::string& what, int code = SPAN_EINVAL) {
+  PyObject* e = PyObject_CallFunction(bound.error, "is", code, (std::string(who) + ": " + what).c_str());
   if (e) PyErr_SetObject(bound.error, e);
   Py_XDECREF(e);
   return nullptr;
@@ -189,6 +189,8 @@ PyObject* entry(const char* who, Py_ssize_t n, Py_ssize_t want, F f) {
     return refuse(who, b.what);
   } catch (const Raised&) {
     return nullptr;
+  } catch (const c10::OutOfMemoryError& e) {
+    return refuse(who, e.what_without_backtrace(), SPAN_ENOMEM);
   } catch (const std::exception& e) {
     return refuse(who, e.what());
   }

@@ -14,7 +14,7 @@ import ctypes
 import struct
 from typing import Optional, Sequence
 
-from ._lib import SPAN_EINVAL, SpanError, _check, load, torch
+from ._lib import SPAN_EINVAL, SPAN_ENOMEM, SpanError, _check, load, torch
 
 SPAN_MAX_DRAFTS = 64
 
@@ -28,8 +28,11 @@ def _scratch(nbytes: int, stream, index: int):
     device = torch.device("cuda", index)
     if isinstance(stream, int):
         stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
-    with torch.cuda.stream(stream):  # freed there by that stream's work, not by the current one's
-        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    try:
+        with torch.cuda.stream(stream):  # freed there by that stream's work, not by the current one's
+            return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    except torch.OutOfMemoryError as e:
+        raise SpanError(SPAN_ENOMEM, f"workspace: {e}") from None
 
 
 _native = None

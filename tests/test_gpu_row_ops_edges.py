@@ -190,3 +190,19 @@ def test_autograd_sees_that_outputs_were_written():
             y.backward()
     with torch.inference_mode():
         spanq.adapter_apply(x, x, ids, a, b, None, torch.empty_like(x))
+
+
+def test_a_workspace_that_does_not_fit_is_an_error_of_memory():
+    """2^18 requests of 64 drafts over 2^22 tokens: a TB of sums, on the current stream and on another one."""
+    n, k, V = 1 << 18, 64, 1 << 22
+    lg = torch.zeros(1, V, device="cuda")
+    d, ua = torch.zeros(n, k, dtype=torch.int32, device="cuda"), torch.zeros(n, k, device="cuda")
+    us, acc = torch.zeros(n, device="cuda"), torch.full((n,), 7, dtype=torch.int32, device="cuda")
+    tok = torch.full((n, k + 1), 7, dtype=torch.int32, device="cuda")
+    assert spanq.verify_workspace(n, k, V) > torch.cuda.get_device_properties(0).total_memory
+    for stream in (None, torch.cuda.Stream()):
+        with pytest.raises(spanq.SpanError) as e:
+            spanq.verify_drafts(lg, d, ua, us, None, acc, tok, stream=stream)
+        assert e.value.code == -2
+    torch.cuda.synchronize()
+    assert bool((acc == 7).all()) and bool((tok == 7).all())

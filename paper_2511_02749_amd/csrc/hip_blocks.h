@@ -10,18 +10,25 @@ namespace spanq {
 class DeviceScope {
  public:
   explicit DeviceScope(int device) {
-    if (device < 0 || hipGetDevice(&before_) != hipSuccess || before_ == device) return;
-    changed_ = hipSetDevice(device) == hipSuccess;
+    if (device < 0) return;
+    error_ = hipGetDevice(&before_);
+    if (error_ != hipSuccess || before_ == device) return;
+    error_ = hipSetDevice(device);
+    changed_ = error_ == hipSuccess;
+    if (!changed_) (void)hipGetLastError();  // returned by error(): not for the next call's check to find
   }
   ~DeviceScope() {
     if (changed_) (void)hipSetDevice(before_);
   }
+  // why `device` is not the current one
+  hipError_t error() const { return error_; }
   DeviceScope(const DeviceScope&) = delete;
   DeviceScope& operator=(const DeviceScope&) = delete;
 
  private:
   int before_ = -1;
   bool changed_ = false;
+  hipError_t error_ = hipSuccess;
 };
 
 struct HipBlocks {

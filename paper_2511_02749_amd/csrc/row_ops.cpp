@@ -93,6 +93,7 @@ int span_qk_norm_rope(const span_qk_norm* args, void* stream) {
   if (what) return bad(who, what);
   if (a.n_rows == 0 || (!a.q && !a.k && !a.v)) return SPAN_OK;
   const DeviceScope device(a.device);
+  if (device.error() != hipSuccess) return done(who, device.error());  // (nothing runs on another one)
   return done(who, launch_qk_norm_rope(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -126,6 +127,7 @@ int span_adapter_apply(const span_adapter_call* args, void* stream) {
   if (a.workspace_bytes < adapter_workspace_bytes(a) || !a.workspace)
     return bad(who, "the workspace is smaller than span_adapter_workspace says");
   const DeviceScope device(a.device);
+  if (device.error() != hipSuccess) return done(who, device.error());  // (nothing runs on another one)
   return done(who, launch_adapter_apply(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -153,6 +155,7 @@ int span_verify_drafts(const span_verify_call* args, void* stream) {
   if (!a.workspace || a.workspace_bytes < verify_workspace_bytes(a.n_requests, a.max_drafts, a.vocab))
     return bad(who, "the workspace is smaller than span_verify_workspace says");
   const DeviceScope device(a.device);
+  if (device.error() != hipSuccess) return done(who, device.error());  // (nothing runs on another one)
   return done(who, launch_verify_drafts(a, static_cast<hipStream_t>(stream)));
 }
 

@@ -206,3 +206,28 @@ def test_a_workspace_that_does_not_fit_is_an_error_of_memory():
         assert e.value.code == -2
     torch.cuda.synchronize()
     assert bool((acc == 7).all()) and bool((tok == 7).all())
+
+
+def test_a_device_that_is_not_there_runs_nothing():
+    """Records of a device that the machine does not have: an error, the current device stays and nothing is written."""
+    from paper_2511_02749_amd import row_ops as R
+    from tests.test_row_ops_refusals import QK_REC
+    lib, bf, there = spanq.load(), torch.bfloat16, torch.cuda.device_count()
+    x, out = torch.ones(2, 64, dtype=bf, device="cuda"), torch.full((2, 64), 7.0, dtype=bf, device="cuda")
+    ids, a, b = torch.zeros(2, dtype=torch.int32, device="cuda"), torch.ones(1, 1, 8, 64, dtype=bf, device="cuda"), torch.ones(1, 64, 8, dtype=bf, device="cuda")
+    ws = torch.empty(spanq.adapter_workspace(2, 64, 8, (64,)) + spanq.verify_workspace(2, 0, 64), dtype=torch.uint8, device="cuda")
+    lg, u = torch.zeros(2, 64, device="cuda"), torch.zeros(2, device="cuda")
+    acc, tok = torch.full((2,), 7, dtype=torch.int32, device="cuda"), torch.full((2, 1), 7, dtype=torch.int32, device="cuda")
+    p = lambda t: t.data_ptr()  # noqa: E731
+    torch.cuda.synchronize()
+    for entry, blob in (
+            ("span_qk_norm_rope", QK_REC.pack(p(x), 0, 0, p(out), 0, 0, 0, 0, 0, 0, 64, 0, 0, 64, 0, 0, 2, 2, 1, 0, 64, 1, there,
+                                              1e-5, 1e4, 0)),
+            ("span_adapter_apply", R._ADAPTER_REC.pack(p(x), p(x), p(out), p(ids), p(a), p(b), 0, 0, p(ws), ws.numel(), 64, 64, 64,
+                                                       2, 64, 1, 8, 1, 64, 0, 0, 0, there, 0)),
+            ("span_verify_drafts", R._VERIFY_REC.pack(p(lg), 0, 0, 0, 0, 0, 0, p(u), 0, p(acc), p(tok), 0, p(ws), ws.numel(), 64,
+                                                      64, 2, 0, 2, 0, 64, there))):
+        assert getattr(lib, entry)(blob, None) == -3 and entry in lib.span_last_error().decode()
+        assert torch.cuda.current_device() == 0
+    torch.cuda.synchronize()
+    assert bool((out == 7).all()) and bool((acc == 7).all()) and bool((tok == 7).all())

@@ -36,6 +36,10 @@ class BlockCache {
   static constexpr size_t kMaxBlocks = 4, kMaxBytes = size_t{256} << 20;
 
   explicit BlockCache(int device) : device_(device) {
+    // room for all there ever are (an event is made when none is spare: one for each kept block, and
+    // one for the block that is given back), so that no give or take fails half way
+    kept_.reserve(kMaxBlocks);
+    spare_.reserve(kMaxBlocks + 1);
     std::lock_guard<std::mutex> lock(all_mu_);
     next_ = first_;
     first_ = this;

@@ -931,6 +931,11 @@ void PoolIndex::rebuild_work(Plan* p, const Tiling& t) {
   build_work(p, t);
 }
 
+// Room in v for n more elements; capacities grow as push_back's do.
+static void make_room(std::vector<int32_t>* v, size_t n) {
+  if (v->capacity() - v->size() < n) v->reserve(std::max(2 * v->capacity(), v->size() + n));
+}
+
 int PoolIndex::decode(Plan* p, const std::vector<int32_t>& n_new, const std::vector<int64_t>& rows,
                       const Tiling& t, std::string* msg) {
   const int32_t ps = page_size_;
@@ -958,6 +963,13 @@ int PoolIndex::decode(Plan* p, const std::vector<int32_t>& n_new, const std::vec
   }
   p->decoded.resize(nq, 0);
   p->stale_tail.resize(nq, 0);
+  // room for every id before a page changes hands: none is lost where memory runs out
+  for (std::vector<int32_t>* ids : {&p->evicted, &p->new_pages, &p->cross_pages}) make_room(ids, static_cast<size_t>(need));
+  for (size_t q = 0; q < nq; ++q) {
+    SpanPlan& cross = p->spans[p->query_spans[q].back()];
+    const size_t pages = static_cast<size_t>((static_cast<int64_t>(cross.n_tok) + n_new[q] + ps - 1) / ps);
+    if (pages > cross.pages.size()) make_room(&cross.pages, pages - cross.pages.size());
+  }
   Plan::DecodeStep& d = p->dec;
   d = Plan::DecodeStep{};
   std::vector<CrossTile> ct;

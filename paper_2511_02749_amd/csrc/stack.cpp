@@ -661,8 +661,31 @@ int span_model_destroy(span_model* m) {
   return SPAN_OK;
 }
 
-int span_model_forward(span_model* m, span_plan_t* plan, const int32_t* row_tokens, int64_t n_rows, int32_t n_layers,
-                       void* hidden_out, float* logits_out, int32_t* first_tokens, void* stream) {
+}  // extern "C"
+
+namespace {
+
+// A decode step that fails appends nothing to the plan.
+struct TakeBack {
+  span_plan_t* plan;
+  const std::vector<int32_t>& n;  // tokens of each query
+  hipStream_t s;
+  bool armed = true;
+  ~TakeBack() {
+    if (!armed) return;
+    (void)hipStreamSynchronize(s);  // what was launched of the step writes no page that is free again
+    try {
+      const std::string why = span_last_error();
+      (void)span_plan_rewind(plan, n.data());
+      (void)report(SPAN_EHIP, why.c_str());
+    } catch (const std::exception&) {
+      (void)span_plan_rewind(plan, n.data());
+    }
+  }
+};
+
+int forward(span_model* m, span_plan_t* plan, const int32_t* row_tokens, int64_t n_rows, int32_t n_layers,
+            void* hidden_out, float* logits_out, int32_t* first_tokens, hipStream_t s) {
   if (!m || !plan || (!row_tokens && n_rows > 0) || n_rows < 0)
     return report(SPAN_EINVAL, "span_model_forward: bad argument");
   if (plan_pool(plan) != m->pool) return report(SPAN_EINVAL, "span_model_forward: the plan belongs to another pool");
@@ -671,7 +694,6 @@ int span_model_forward(span_model* m, span_plan_t* plan, const int32_t* row_toke
     return report(SPAN_EINVAL, "span_model_forward: n_layers must lie in [0, num_layers]");
   if ((first_tokens || logits_out) && n_layers != c.num_layers)
     return report(SPAN_EINVAL, "span_model_forward: the LM head needs every layer");
-  hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = hipSetDevice(m->device);
   if (e != hipSuccess) return hip_err(e, "span_model_forward: hipSetDevice");
 
@@ -759,8 +781,8 @@ int span_model_forward(span_model* m, span_plan_t* plan, const int32_t* row_toke
   return SPAN_OK;
 }
 
-int span_model_decode(span_model* m, span_plan_t* plan, const int32_t* tokens, float* logits_out, int32_t* next_tokens,
-                      void* stream) {
+int decode(span_model* m, span_plan_t* plan, const int32_t* tokens, float* logits_out, int32_t* next_tokens,
+           hipStream_t s) {
   if (!m || !plan) return report(SPAN_EINVAL, "span_model_decode: null argument");
   if (plan_pool(plan) != m->pool) return report(SPAN_EINVAL, "span_model_decode: the plan belongs to another pool");
   const span_model_config& c = m->cfg;
@@ -778,7 +800,6 @@ int span_model_decode(span_model* m, span_plan_t* plan, const int32_t* tokens, f
     rows[qi] = static_cast<int64_t>(q_of.size());
     q_of.push_back(qi);
   }
-  hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t e = hipSetDevice(m->device);
   if (e != hipSuccess) return hip_err(e, "span_model_decode: hipSetDevice");
   if (next_tokens)
@@ -789,6 +810,7 @@ int span_model_decode(span_model* m, span_plan_t* plan, const int32_t* tokens, f
   int rc = check_adapters(m, adapters, "span_model_decode");
   if (!rc) rc = span_plan_decode(plan, n_new.data(), rows.data(), s);
   if (rc) return rc;
+  TakeBack take_back{plan, n_new, s};
   // one compact row per decoding query; its attention row is the same index
   int32_t* h_rows = nullptr;
   rc = stage_area(m, 4 * static_cast<size_t>(nd) + 8, &h_rows, "span_model_decode");
@@ -809,18 +831,14 @@ int span_model_decode(span_model* m, span_plan_t* plan, const int32_t* tokens, f
   rc = run_layers(m, nd, c.num_layers, 0, nd, ad, s, "span_model_decode",
                   [&](int l) { return span_decode_attend(plan, l, m->q.p, m->k.p, m->v.p, m->o.p, s); });
   if (rc) return rc;
-  if (!next_tokens && !logits_out) return SPAN_OK;
   std::vector<int32_t> toks;
-  rc = lm_head(m, nd, logits_out, next_tokens ? &toks : nullptr, s, "span_model_decode");
+  if (next_tokens || logits_out) rc = lm_head(m, nd, logits_out, next_tokens ? &toks : nullptr, s, "span_model_decode");
   if (rc) return rc;
+  take_back.armed = false;
   if (next_tokens)
     for (int i = 0; i < nd; ++i) next_tokens[q_of[i]] = toks[i];
   return SPAN_OK;
 }
-
-}  // extern "C"
-
-namespace {
 
 // Fills a layer table from a caller's (null: empty).
 void take_table(const void* const* t, int layers, std::vector<const void*>* to) {
@@ -918,18 +936,7 @@ int decode_drafts(span_model* m, span_plan_t* plan, const int32_t* tokens, const
   if (e != hipSuccess) return hip_err(e, std::string(who) + ": hipSetDevice");
   rc = span_plan_decode(plan, n_new.data(), rows.data(), s);
   if (rc) return rc;
-  // a step that fails leaves the plan as it was
-  struct TakeBack {
-    span_plan_t* plan;
-    const std::vector<int32_t>& n;
-    bool armed = true;
-    ~TakeBack() {
-      if (!armed) return;
-      const std::string why = span_last_error();
-      (void)span_plan_rewind(plan, n.data());
-      (void)report(SPAN_EHIP, why.c_str());
-    }
-  } take_back{plan, n_new};
+  TakeBack take_back{plan, n_new, s};
   // staging: the row lists, then verification's inputs (drafts, u_accept: [nd][k]; n_drafts,
   // first rows, u_sample, temperature: [nd])
   const int64_t n_in = nd * (2 * static_cast<int64_t>(k) + 5);
@@ -1022,16 +1029,18 @@ int decode_drafts(span_model* m, span_plan_t* plan, const int32_t* tokens, const
   if (e == hipSuccess) e = hipStreamSynchronize(s);
   if (e != hipSuccess) return hip_err(e, std::string(who) + ": tokens");
   std::vector<int32_t> drop(static_cast<size_t>(nq), 0);
+  for (int i = 0; i < nd; ++i) drop[q_of[i]] = in_n[i] - out[i];
+  rc = span_plan_rewind(plan, drop.data());
+  if (rc) return rc;
   take_back.armed = false;
   for (int i = 0; i < nd; ++i) {
     const int qi = q_of[i];
     n_out[qi] = out[i] + 1;
-    drop[qi] = in_n[i] - out[i];
     const int32_t* t = out.data() + nd + i * k1;
     std::copy(t, t + k1, out_tokens + qi * k1);
     if (logprobs) std::memcpy(logprobs + qi * k1, out.data() + nd + (nd + i) * k1, static_cast<size_t>(k1) * 4);
   }
-  return span_plan_rewind(plan, drop.data());
+  return SPAN_OK;
 }
 
 // No C++ exception leaves the C entries: what they throw is a failed allocation.
@@ -1047,6 +1056,21 @@ int no_throw(const char* who, F f) {
 }  // namespace
 
 extern "C" {
+
+int span_model_forward(span_model* m, span_plan_t* plan, const int32_t* row_tokens, int64_t n_rows, int32_t n_layers,
+                       void* hidden_out, float* logits_out, int32_t* first_tokens, void* stream) {
+  return no_throw("span_model_forward", [&] {
+    return forward(m, plan, row_tokens, n_rows, n_layers, hidden_out, logits_out, first_tokens,
+                   static_cast<hipStream_t>(stream));
+  });
+}
+
+int span_model_decode(span_model* m, span_plan_t* plan, const int32_t* tokens, float* logits_out, int32_t* next_tokens,
+                      void* stream) {
+  return no_throw("span_model_decode", [&] {
+    return decode(m, plan, tokens, logits_out, next_tokens, static_cast<hipStream_t>(stream));
+  });
+}
 
 int span_model_set_qk_norm(span_model* m, const void* const* q_norm, const void* const* k_norm) {
   if (!m) return report(SPAN_EINVAL, "span_model_set_qk_norm: null model");

@@ -1,125 +1,8 @@
 // Decode steps whose calls of the device runtime fail, one after another: nothing is appended, and the
-// step can be planned again.  The runtime is this program's own, on host memory (its symbols come before
-// the library's runtime), and no kernel runs.
-#include <cstdio>
-#include <cstdlib>
-#include <cstring>
-#include <vector>
-
-#include "spanq.h"
+// step can be planned again.
+#include "told_runtime.h"
 
 namespace {
-int fail_in = -1;  // calls until one fails, -1: none does
-int calls = 0;     // that could have failed
-int live = 0;      // device allocations
-constexpr int kError = 2;  // out of memory
-
-int step() {
-  ++calls;
-  if (fail_in < 0) return 0;
-  return fail_in-- == 0 ? kError : 0;
-}
-int make(void** p, size_t n) {
-  const int e = step();
-  if (e) return e;
-  *p = std::malloc(n ? n : 1);
-  ++live;
-  return 0;
-}
-int drop(void* p) {
-  if (p) --live;
-  std::free(p);
-  return 0;
-}
-}  // namespace
-
-extern "C" {
-int hipSetDevice(int) { return step(); }
-int hipGetDevice(int* d) { return *d = 0; }
-int hipDeviceGetAttribute(int* v, int, int) { return *v = 0; }
-int hipDeviceGetDefaultMemPool(void** p, int) { *p = nullptr; return 0; }
-int hipMemPoolSetAttribute(void*, int, void*) { return 0; }
-int hipDeviceSynchronize() { return 0; }
-int hipMalloc(void** p, size_t n) { return make(p, n); }
-int hipFree(void* p) { return drop(p); }
-int hipMallocAsync(void** p, size_t n, void*) { return make(p, n); }
-int hipFreeAsync(void* p, void*) { return drop(p); }
-int hipMemcpy(void* to, const void* from, size_t n, int) {
-  std::memcpy(to, from, n);
-  return 0;
-}
-int hipMemcpyAsync(void* to, const void* from, size_t n, int, void*) {
-  const int e = step();
-  if (!e) std::memcpy(to, from, n);
-  return e;
-}
-int hipEventCreateWithFlags(void** e, unsigned) {
-  *e = nullptr;
-  const int r = step();
-  if (!r) *e = std::malloc(1);
-  return r;
-}
-int hipEventCreate(void** e) { return hipEventCreateWithFlags(e, 0); }
-int hipEventDestroy(void* e) {
-  std::free(e);
-  return 0;
-}
-int hipEventRecord(void*, void*) { return step(); }
-int hipEventSynchronize(void*) { return step(); }
-int hipEventQuery(void*) { return 0; }
-int hipStreamSynchronize(void*) { return 0; }
-int hipStreamWaitEvent(void*, void*, unsigned) { return step(); }
-int hipStreamIsCapturing(void*, int* s) { return *s = 0; }
-int hipThreadExchangeStreamCaptureMode(int*) { return 0; }
-int hipGetLastError() { return 0; }
-const char* hipGetErrorString(int) { return "told to fail"; }
-int hipFuncSetAttribute(const void*, int, int) { return 0; }
-int hipGetSymbolAddress(void** p, const void*) {
-  static char there[1 << 20];
-  *p = there;
-  return 0;
-}
-int hipLaunchKernel(const void*, unsigned long long, unsigned, unsigned long long, unsigned, void**, size_t, void*) { return 0; }
-}
-
-namespace {
-
-#define CHECK(x)                                                                     \
-  do {                                                                               \
-    if (!(x)) {                                                                      \
-      std::fprintf(stderr, "line %d: %s (%s)\n", __LINE__, #x, span_last_error());  \
-      std::exit(1);                                                                  \
-    }                                                                                \
-  } while (0)
-
-struct Seen {
-  std::vector<int32_t> pages[2];
-  int64_t free_pages, pinned, steps, tokens, decode_pages;
-  bool operator==(const Seen& o) const {
-    return pages[0] == o.pages[0] && pages[1] == o.pages[1] && free_pages == o.free_pages && pinned == o.pinned &&
-           steps == o.steps && tokens == o.tokens && decode_pages == o.decode_pages;
-  }
-};
-
-Seen look(span_pool* pool, span_plan_t* plan) {
-  Seen s{};
-  for (int q = 0; q < 2; ++q) {
-    int32_t n = 0, hit = 0;
-    s.pages[q].resize(64);
-    CHECK(span_plan_block_table(plan, q, q == 0 ? 1 : 0, s.pages[q].data(), 64, &n, &hit) == SPAN_OK);
-    s.pages[q].resize(n);
-  }
-  span_pool_info i{};
-  CHECK(span_pool_get_info(pool, &i) == SPAN_OK);
-  span_stats st{};
-  CHECK(span_plan_stats(plan, &st) == SPAN_OK);
-  s.free_pages = i.free_pages;
-  s.pinned = i.pinned_pages;
-  s.steps = st.decode_steps;
-  s.tokens = st.decode_tokens;
-  s.decode_pages = st.decode_pages;
-  return s;
-}
 
 // Steps of one plan, each tried with every call of the runtime failing in turn before it is let through.
 int run(int dtype, void* other_stream) {
@@ -137,13 +20,13 @@ int run(int dtype, void* other_stream) {
   CHECK(span_pool_create(&cfg, &pool) == SPAN_OK);
   std::vector<int32_t> tok(64);
   for (int i = 0; i < 64; ++i) tok[i] = i;
-  span_tokens frag{tok.data(), 5, 20};
+  span_tokens frag{tok.data(), 5, 0, 20};
   span_query q[2] = {};
-  q[0].prefix = span_tokens{tok.data(), 17, 0};
+  q[0].prefix = span_tokens{tok.data(), 17, 0, 0};
   q[0].frags = &frag;
   q[0].n_frags = 1;
-  q[0].cross = span_tokens{tok.data() + 30, 13, 30};
-  q[1].cross = span_tokens{tok.data() + 50, 3, 50};
+  q[0].cross = span_tokens{tok.data() + 30, 13, 0, 30};
+  q[1].cross = span_tokens{tok.data() + 50, 3, 0, 50};
   span_plan_t* plan = nullptr;
   CHECK(span_plan(pool, q, 2, nullptr, &plan) == SPAN_OK);
   const Seen first = look(pool, plan);

@@ -44,7 +44,16 @@ const char* check_part(const void* in, const void* out, const void* gain, int64_
   return nullptr;
 }
 
-const char* check_adapter_sizes(const span_adapter_call& a) {
+const char* check_verify_sizes(const span_verify_call& a) {
+  if (a.n_requests < 0 || a.n_requests > kMaxWide) return "n_requests must lie in [0, 2^20]";
+  if (a.max_drafts < 0 || a.max_drafts > SPAN_MAX_DRAFTS) return "max_drafts must lie in [0, SPAN_MAX_DRAFTS]";
+  if (a.vocab < 1 || a.vocab > (1 << 24)) return "vocab must lie in [1, 2^24]";
+  return nullptr;
+}
+
+}  // namespace
+
+const char* spanq::check_adapter_sizes(const span_adapter_call& a) {
   if (a.n_rows < 0 || a.n_rows > kMaxRows) return "n_rows must lie in [0, 2^31)";
   if (a.in_features < 8 || a.in_features % 8 != 0 || a.in_features > kMaxWide)
     return "in_features must be a multiple of 8 in [8, 2^20]";
@@ -58,15 +67,6 @@ const char* check_adapter_sizes(const span_adapter_call& a) {
   if (n > kMaxWide) return "the parts' columns must be at most 2^20 together";
   return nullptr;
 }
-
-const char* check_verify_sizes(const span_verify_call& a) {
-  if (a.n_requests < 0 || a.n_requests > kMaxWide) return "n_requests must lie in [0, 2^20]";
-  if (a.max_drafts < 0 || a.max_drafts > SPAN_MAX_DRAFTS) return "max_drafts must lie in [0, SPAN_MAX_DRAFTS]";
-  if (a.vocab < 1 || a.vocab > (1 << 24)) return "vocab must lie in [1, 2^24]";
-  return nullptr;
-}
-
-}  // namespace
 
 extern "C" {
 

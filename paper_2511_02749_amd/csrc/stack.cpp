@@ -303,7 +303,7 @@ int add_adapter(span_model* m, int proj, int l, const AdaptedRows& ad, const voi
   return span_adapter_apply(&a, s);
 }
 
-// Does any of the plan's ids not exist, or does any exist at all?
+// SPAN_EINVAL if one of the plan's ids does not exist.
 int check_adapters(const span_model* m, const std::vector<int32_t>& ids, const char* who) {
   for (int32_t id : ids)
     if (id >= m->n_adapters)
@@ -875,6 +875,11 @@ int set_adapters(span_model* m, const span_model_adapters* a) {
         ok = !at[p][l] == !bt[p][l] && reinterpret_cast<uintptr_t>(at[p][l]) % 16 == 0 &&
              reinterpret_cast<uintptr_t>(bt[p][l]) % 16 == 0;
       if (!ok) return report(SPAN_EINVAL, "span_model_set_adapters: a and b go together, 16-byte aligned");
+      if (!at[p]) continue;
+      span_adapter_call c = adapter_call(m, p);
+      c.max_rank = a->max_rank;
+      if (const char* what = check_adapter_sizes(c))
+        return report(SPAN_EINVAL, (std::string("span_model_set_adapters: ") + what).c_str());
     }
   }
   for (int p = 0; p < 4; ++p) {

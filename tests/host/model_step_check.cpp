@@ -128,6 +128,14 @@ int main() {
     CHECK(span_plan_destroy(plan) == SPAN_OK);
   }
   CHECK(span_model_destroy(model) == SPAN_OK);
+
+  // products wider than the operator takes are refused when they are given, not in the middle of a forward
+  mc.ffn = (1 << 19) + 8;
+  CHECK(span_model_create(pool, &mc, &model) == SPAN_OK);
+  CHECK(span_model_set_adapters(model, &ad) == SPAN_OK);  // (down: a long reduction)
+  ad.a_gate_up = ad.b_gate_up = table;
+  CHECK(span_model_set_adapters(model, &ad) == SPAN_EINVAL);
+  CHECK(span_model_destroy(model) == SPAN_OK);
   CHECK(span_pool_destroy(pool) == SPAN_OK);
   CHECK(failed > 300 && live == 0);
   std::printf("%d failures\nall checks passed\n", failed);

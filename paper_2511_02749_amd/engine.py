@@ -23,6 +23,7 @@ from typing import List, Optional, Sequence
 import numpy as np
 
 from . import spanquery as sq
+from ._lib import SPAN_ENOMEM, SpanError
 
 
 @dataclass
@@ -131,6 +132,13 @@ class Engine:
                           tokens)
             return tokens[:, 0].tolist()
 
+    def _step(self, plan, out, open_, drafts):
+        n = len(out)
+        return self.model.decode_drafts(
+            plan, [o[-1] if go else -1 for o, go in zip(out, open_)], drafts,
+            u_accept=[self._rng.random(len(d), np.float32) for d in drafts], u_sample=self._rng.random(n, np.float32),
+            temperature=np.full(n, self.temperature, np.float32), stream=self.stream)
+
     def _decode_checked(self, plan, history, out, max_tokens: int):
         """Steps of drafts and sampled tokens until every query has max_tokens; (drafts fed, kept)."""
         n, fed, kept = len(out), 0, 0
@@ -142,11 +150,13 @@ class Engine:
             open_ = [len(o) < max_tokens for o in out]
             drafts = [lookup_drafts(s[:len(h) + len(o)], min(self.n_drafts, max_tokens - len(o) - 1)) if go else []
                       for s, h, o, go in zip(seen, history, out, open_)]
-            got = self.model.decode_drafts(
-                plan, [o[-1] if go else -1 for o, go in zip(out, open_)], drafts,
-                u_accept=[self._rng.random(len(d), np.float32) for d in drafts],
-                u_sample=self._rng.random(n, np.float32), temperature=np.full(n, self.temperature, np.float32),
-                stream=self.stream)
+            try:
+                got = self._step(plan, out, open_, drafts)
+            except SpanError as e:
+                if e.code != SPAN_ENOMEM or not any(drafts):
+                    raise
+                drafts = [[]] * n  # no pages for drafted tokens: a step without them needs fewer
+                got = self._step(plan, out, open_, drafts)
             _check_weight(t for g in got for t in g)
             fed += sum(len(d) for d in drafts)
             kept += sum(len(g) - 1 for g in got if g)

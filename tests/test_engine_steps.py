@@ -1,6 +1,7 @@
 """Steps of the generation engine with drafts and sampling, on the CPU with a model that is told its answers."""
 import pytest
 
+from paper_2511_02749_amd import SpanError
 from paper_2511_02749_amd import spanquery as sq
 from paper_2511_02749_amd.engine import Engine
 
@@ -11,7 +12,7 @@ class _Told:
     def __init__(self, first, steps=()):
         self.first, self.steps = first, list(steps)
         self.committed = self.destroyed = False
-        self.fed = []
+        self.fed, self.drafts = [], []
 
     def plan(self, queries, stream):
         return self
@@ -21,7 +22,11 @@ class _Told:
 
     def decode_drafts(self, plan, tokens, drafts, **_):
         self.fed.append(list(tokens))
-        return self.steps.pop(0)
+        self.drafts.append([list(d) for d in drafts])
+        step = self.steps.pop(0)
+        if isinstance(step, Exception):
+            raise step
+        return step
 
     def stats(self):
         return dict(pages_hit=0, tokens_hit=0, tokens_new=0, decode_steps=len(self.fed))
@@ -72,3 +77,15 @@ def test_finished_queries_feed_nothing_and_the_others_go_on():
     told = _Told([7, 8], [[[5, 6], [9]], [[], [4]]])
     assert Engine(told, told, n_drafts=2).generate_many(_spans(2), 3) == [[7, 5, 6], [8, 9, 4]]
     assert told.committed and told.fed == [[7, 8], [-1, 9]]
+
+
+def test_drafts_that_the_pool_has_no_pages_for_are_left_out():
+    spans = [sq.Spans(prefix=[], fragments=[], cross=[7, 3, 4, 5, 7])]
+    told = _Told([3], [SpanError(-2, "pages"), [[4]], [[5, 7]]])
+    assert Engine(told, told, n_drafts=4).generate_many(spans, 4) == [[3, 4, 5, 7]]
+    assert told.drafts == [[[4, 5]], [[]], [[5]]] and told.committed
+    for error, steps in ((SpanError(-2, "pages"), 2), (SpanError(-3, "runtime"), 1)):
+        told = _Told([3], [error] * steps)
+        with pytest.raises(SpanError):
+            Engine(told, told, n_drafts=4).generate_many(spans, 4)
+        assert not told.steps and told.destroyed and not told.committed

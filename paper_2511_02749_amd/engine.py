@@ -24,6 +24,7 @@ import numpy as np
 
 from . import spanquery as sq
 from ._lib import SPAN_ENOMEM, SpanError
+from .row_ops import SPAN_MAX_DRAFTS
 
 
 @dataclass
@@ -65,11 +66,13 @@ class Engine:
     model: object                      # paper_2511_02749_amd.Model on that pool
     stream: object = None
     calls: List[CallStats] = field(default_factory=list)
-    n_drafts: int = 0                  # drafted tokens that a decode step checks, 0: none
+    n_drafts: int = 0                  # drafted tokens that a decode step checks, at most SPAN_MAX_DRAFTS; 0: none
     temperature: float = 0.0           # 0: greedy
     seed: int = 0
 
     def __post_init__(self):
+        if not 0 <= self.n_drafts <= SPAN_MAX_DRAFTS:
+            raise ValueError(f"n_drafts must lie in [0, {SPAN_MAX_DRAFTS}]")
         self._rng = np.random.default_rng(self.seed)
 
     def generate_many(self, spans: Sequence[sq.Spans], max_tokens: int,

@@ -89,3 +89,10 @@ def test_drafts_that_the_pool_has_no_pages_for_are_left_out():
         with pytest.raises(SpanError):
             Engine(told, told, n_drafts=4).generate_many(spans, 4)
         assert not told.steps and told.destroyed and not told.committed
+
+
+@pytest.mark.parametrize("n", [-1, 65, 1000])
+def test_numbers_of_drafts_that_no_step_takes_are_refused_at_once(n):
+    with pytest.raises(ValueError, match="n_drafts"):
+        Engine(None, None, n_drafts=n)
+    assert Engine(None, None, n_drafts=64).n_drafts == 64

@@ -168,11 +168,6 @@ __device__ __forceinline__ void multiply_h(const uint4& h, const uint4 (&w)[J], 
     acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(h), as_frag(w[j]), acc[j], 0, 0, 0);
 }
 
-// A block of ranks of one row of H, as two operands.
-struct HRow {
-  uint4 first, low;
-};
-
 // Eight weights, infinite ones and NaN replaced by 0.  An infinite weight times H is what it is times H's
 // high part, which has H's sign and is 0 only where H is; a middle or low part may be 0 or of the
 // other sign and would make it NaN.
@@ -333,12 +328,14 @@ __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Sh
       }
       multiply();
     }
-    // A lane holds ranks 4 g .. of row m of each tile.  All tiles are stored, those past the last one too: no
-    // condition stands between a matrix instruction and the store of its result.
+    // A lane holds ranks 4 g .. of row m of each tile.  Stores of matrix instructions' results stand behind a
+    // condition here (all four tiles stored: 1 us more for one): their wait is spelled out.
+    asm volatile("s_nop 15" ::: "memory");
 #pragma unroll
     for (int t = 0; t < C::kRows; ++t)
 #pragma unroll
-      for (int c = 0; c < C::kCols; ++c) red[wave][c][16 * t + m][g] = __builtin_bit_cast(float4, acc[t][c]);
+      for (int c = 0; c < C::kCols; ++c)
+        if (c < n_ct) red[wave][c][16 * t + m][g] = __builtin_bit_cast(float4, acc[t][c]);
     __syncthreads();
     for (int e = threadIdx.x; e < n_ct * 64 * C::kRows; e += 64 * C::kWaves) {
       const int q = e & 3, row = (e >> 2) % (16 * C::kRows), c = e / (64 * C::kRows);
@@ -453,21 +450,36 @@ struct Out {
     return v;
   }
   // The tiles' results once more, where one is infinite or NaN: only H's high parts meet infinite weights.
+  // h(rb, at): vector `at` of block rb of the lane's row of H.  With kPairs the low parts of two
+  // blocks go together.  The steps are those of the first time, so that finite results keep their bits.
   // (The weights are fetched again: kept for this, they would cost registers that every call has to give.)
-  template <class F>
-  static __device__ __forceinline__ void wild(const Shape& s, const Cols& c, int aid, int rank, int m, int g, F h_of,
+  template <bool kPairs, class F>
+  static __device__ __forceinline__ void wild(const Shape& s, const Cols& c, int aid, int rank, int m, int g, F h,
                                               f32x4_t (&acc)[J]) {
 #pragma unroll
     for (int j = 0; j < J; ++j) acc[j] = f32x4_t{};
-#pragma unroll 1
-    for (int rb = 0; 16 * rb < rank; ++rb) {
-      const HRow h = h_of(rb);
+    auto weight = [&](int rb, int j) { return weights(s, c, aid, j, m, 16 * rb + 8 * (g & 1), rank, false); };
+    auto multiply = [](const uint4& h, const uint4& w, f32x4_t& sum) {
+      sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(h), as_frag(w), sum, 0, 0, 0);
+    };
+    auto first = [&](int rb) {
+      const uint4 part = h(rb, g);
 #pragma unroll
       for (int j = 0; j < J; ++j) {
-        const int r0 = 16 * rb + 8 * (g & 1);
-        const uint4 w = weights(s, c, aid, j, m, r0, rank, false), finite = finite_of(w);
-        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(h.low), as_frag(finite), acc[j], 0, 0, 0);
-        acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(h.first), as_frag(g < 2 ? w : finite), acc[j], 0, 0, 0);
+        const uint4 w = weight(rb, j), finite = finite_of(w);
+        multiply(part, g < 2 ? w : finite, acc[j]);
+      }
+    };
+#pragma unroll 1
+    for (int rb = 0; 16 * rb < rank; rb += kPairs ? 2 : 1) {
+      if constexpr (!kPairs) first(rb);
+      const int mine = kPairs ? rb + (g >> 1) : rb;
+      const uint4 low = kPairs || g < 2 ? h(mine, 4 + (g & 1)) : uint4{0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int j = 0; j < J; ++j) multiply(low, finite_of(weight(mine, j)), acc[j]);
+      if constexpr (kPairs) {
+        first(rb);
+        if (16 * rb + 16 < rank) first(rb + 1);
       }
     }
   }
@@ -501,7 +513,7 @@ unsigned col_blocks(const Shape& s) {
 // B): 7.5 us; 777 ordered rows of 2048 columns: 6.4.
 constexpr int kTileJ = 4;
 template <bool kFew>
-__global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(const Shape s) {
+__global__ __launch_bounds__(64 * kExpandWaves, kFew ? 5 : 3) void adapter_expand_tile_kernel(const Shape s) {
   constexpr int J = kTileJ;
   using O = Out<J, false>;
   __shared__ int list[kTile];
@@ -590,14 +602,11 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(
     const float scale = s.scale ? s.scale[id] : 1.f;
     if (!formed) form();
     formed = true;
-    // of H, ranks 8 (g & 1) .. of a block: high (g < 2) or middle parts, then low ones or nothing
-    auto h_of = [&](int rb) {
-      const uint4* h = reinterpret_cast<const uint4*>(hs[rb][min(m, count - 1)]) + g;
-      return HRow{h[0], g < 2 ? h[4] : uint4{0u, 0u, 0u, 0u}};
-    };
+    auto load_h = [&](int rb, int at) { return reinterpret_cast<const uint4*>(hs[rb][min(m, count - 1)])[at]; };
     f32x4_t acc[J] = {};
     for (int rb = 0; 16 * rb < rank; ++rb) {
-      const HRow h = h_of(rb);
+      // of H, ranks 8 (g & 1) .. of the block: high (g < 2) or middle parts, then low ones or nothing
+      const uint4 first = load_h(rb, g), low = g < 2 ? load_h(rb, 4 + g) : uint4{0u, 0u, 0u, 0u};
       if (16 * rb + 16 > rank) {
 #pragma unroll
         for (int j = 0; j < J; ++j) wv[j] = first_of(wv[j], rank - 16 * rb - 8 * (g & 1));
@@ -605,12 +614,12 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(
       uint4 next[J];
 #pragma unroll
       for (int j = 0; j < J; ++j) next[j] = O::weights(s, cols, id, j, m, 16 * (rb + 1) + 8 * (g & 1), 0, true);
-      multiply_h(h.first, wv, acc);
-      multiply_h(h.low, wv, acc);
+      multiply_h(first, wv, acc);
+      multiply_h(low, wv, acc);
 #pragma unroll
       for (int j = 0; j < J; ++j) wv[j] = next[j];
     }
-    if (__builtin_expect(any_wild(acc), 0)) O::wild(s, cols, id, rank, m, g, h_of, acc);
+    if (__builtin_expect(any_wild(acc), 0)) O::template wild<false>(s, cols, id, rank, m, g, load_h, acc);
     put(mine, [&](int i) { return O::add(bv[i], acc, i, scale); });
     if constexpr (kFew) return;
   }
@@ -626,8 +635,10 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_tile_kernel(
 constexpr int kManyJ = 4;
 constexpr int kManyRun = 8;  // at most
 constexpr int kShortRun = 2;
+// (Two blocks kept: three waves a SIMD, at most 168 registers. `wild` would have the compiler take 176: 79 us for 75 for
+// 2048 rows of 28672 columns in all.)
 template <int kKept, int kRun>
-__global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(const Shape s) {
+__global__ __launch_bounds__(64 * kExpandWaves, kKept == 2 ? 3 : 1) void adapter_expand_many_kernel(const Shape s) {
   constexpr int J = kManyJ;
   using O = Out<J, true>;
   const int lane = threadIdx.x & 63;
@@ -713,12 +724,8 @@ __global__ __launch_bounds__(64 * kExpandWaves) void adapter_expand_many_kernel(
       multiply_h(load_h(16 * t + m, k, g), wv[k], acc);
       if (16 * k + 16 < rank) multiply_h(load_h(16 * t + m, k + 1, g), wv[k + 1], acc);
     }
-    if (__builtin_expect(any_wild(acc), 0)) {
-      auto h_of = [&](int rb) {
-        return HRow{load_h(16 * t + m, rb, g), g < 2 ? load_h(16 * t + m, rb, 4 + g) : uint4{0u, 0u, 0u, 0u}};
-      };
-      O::wild(s, cols, kept, rank, m, g, h_of, acc);
-    }
+    if (__builtin_expect(any_wild(acc), 0))
+      O::template wild<true>(s, cols, kept, rank, m, g, [&](int rb, int at) { return load_h(16 * t + m, rb, at); }, acc);
   };
   // The usual run, whole and of one adapter, in a loop without a condition on a load or
   // store: each would make the next wait for all of them, stores included.

@@ -91,6 +91,26 @@ def test_adapters_with_infinite_weights(T, N, R):
     assert torch.equal(out[~rest].double().nan_to_num(7.0, 8.0, 9.0), want[~rest].nan_to_num(7.0, 8.0, 9.0))
 
 
+@pytest.mark.parametrize("T,N", FORMS)
+@pytest.mark.parametrize("R", [8, 24, 128])
+def test_rows_of_an_adapter_keep_their_bits_beside_a_row_that_is_no_number(T, N, R):
+    """Every eleventh row of x holds a NaN or an infinity: the others' results are the same bits."""
+    g, K, bf = _gen(T + R), 264, torch.bfloat16
+    x, base, a, b = (torch.randn(*s, generator=g).to(bf).cuda() for s in ((T, K), (T, N), (2, 1, R, K), (2, N, R)))
+    ids = (torch.arange(T) * 3 // 2 % 3 - 1).to(torch.int32).cuda()
+    out, hurt = (torch.full((T, N), 5.0, dtype=bf, device="cuda") for _ in range(2))
+    spanq.adapter_apply(x, base, ids, a, b, None, out)
+    x[::11, 7] = float("nan")
+    x[::22, 7] = float("inf")
+    print(f"beside no numbers T {T} N {N} R {R}", flush=True)
+    spanq.adapter_apply(x, base, ids, a, b, None, hurt)
+    fine = torch.ones(T, dtype=torch.bool, device="cuda")
+    fine[::11] = False
+    assert torch.equal(hurt[fine], out[fine])
+    wild = ~fine & (ids >= 0)
+    assert not bool(hurt[wild].isfinite().all(1).any()) and bool(out.isfinite().all())
+
+
 # ------------------------------------------------------------------------ verification
 
 @pytest.mark.parametrize("V,n", [(1500, 60), (3000, 60), (40000, 40), (128256, 20)])

@@ -340,14 +340,15 @@ PyObject* verify_drafts(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     if (n > INT32_MAX || k > INT32_MAX || vocab > INT32_MAX) throw Bad{"sizes must be below 2^31"};
     const Rows rt = rows_of("target_logits", *target, at::kFloat, gpu, target->sizes());
     span_verify_call c{};
-    c.target_logits = static_cast<const float*>(rt.at);
+    // (a tensor of no rows may have no address, which would say that there is none: any other, never read)
+    c.target_logits = static_cast<const float*>(rt.at ? rt.at : address(tokens));
     c.target_stride = rt.stride;
     c.target_rows = target->size(0);
     c.draft_stride = vocab;
     if (const at::Tensor* draft = tensor("draft_logits", a[7])) {
       if (draft->dim() != 2) throw Bad{"draft_logits must be [rows, vocab]"};
       const Rows rd = rows_of("draft_logits", *draft, at::kFloat, gpu, {draft->size(0), vocab});
-      c.draft_logits = static_cast<const float*>(rd.at);
+      c.draft_logits = static_cast<const float*>(rd.at ? rd.at : address(tokens));
       c.draft_stride = rd.stride;
       c.draft_rows = draft->size(0);
     }

@@ -187,6 +187,23 @@ def test_rotations_by_the_angle_and_not_by_a_float_next_to_it(dim, theta):
     assert bool((err <= bound).all())
 
 
+def test_logits_without_any_rows_are_not_logits_that_were_not_given():
+    """Requests whose rows lie outside logits of no rows at all: -1, as outside any others; requests without drafts
+    need no draft rows."""
+    n, k, V = 4, 2, 100
+    lg, none = torch.randn(n * (k + 1), V, device="cuda"), torch.empty(0, V, device="cuda")
+    d, ua = torch.ones(n, k, dtype=torch.int32, device="cuda"), torch.zeros(n, k, device="cuda")
+    us, heat = torch.rand(n, device="cuda"), torch.ones(n, device="cuda")
+    for target, draft, counts, outside in ((lg, none, None, [1, 1, 1, 1]), (lg, none, [0, 2, 0, 1], [0, 1, 0, 1]),
+                                           (none, None, None, [1, 1, 1, 1]), (none, none, [0, 0, 0, 0], [1, 1, 1, 1])):
+        acc, tok = torch.full((n,), 9, dtype=torch.int32, device="cuda"), torch.full((n, k + 1), 9, dtype=torch.int32, device="cuda")
+        spanq.verify_drafts(target, d, ua, us, heat, acc, tok, draft_logits=draft,
+                            n_drafts=None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda"))
+        for i, out in enumerate(outside):
+            assert int(acc[i]) == (-1 if out else 0), (counts, i)
+            assert bool((tok[i] == -1).all()) if out else 0 <= int(tok[i, 0]) < V
+
+
 # ------------------------------------------------------------------------ tensors
 
 def test_autograd_sees_that_outputs_were_written():

@@ -123,6 +123,14 @@ void* pointer(PyObject* o) {
 // The stream of a call: an address, an object that has one, or None: the GPU's current one.
 void* stream_of(PyObject* o, int gpu) {
   if (PyLong_Check(o)) return pointer(o);
+  if (o != Py_None) {
+    PyObject* of = PyObject_GetAttrString(o, "device_index");  // (not every object with a stream tells)
+    if (!of) PyErr_Clear();
+    const long index = of ? PyLong_AsLong(of) : gpu;
+    Py_XDECREF(of);
+    if (index == -1 && PyErr_Occurred()) throw Raised{};
+    if (index != gpu) throw Bad{"the stream is GPU " + std::to_string(index) + "'s, the tensors lie on " + std::to_string(gpu)};
+  }
   const Ref r(o == Py_None ? PyObject_CallFunction(bound.raw_stream, "i", gpu) : PyObject_GetAttrString(o, "cuda_stream"));
   return pointer(r.p);
 }
@@ -318,10 +326,10 @@ PyObject* adapter_apply(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     c.n_parts = static_cast<int32_t>(n_parts);
     for (int p = 0; p < 4; ++p) c.part_cols[p] = static_cast<int32_t>(parts[p]);
     c.device = gpu;
+    void* stream = stream_of(a[10], gpu);
     const Workspace ws(a[9], gpu, a[10], a[9] == Py_None ? adapter_bytes(c) : 0);
     c.workspace = ws.at;
     c.workspace_bytes = ws.bytes;
-    void* stream = stream_of(a[10], gpu);
     launch([&] { return bound.adapter_apply(&c, stream); });
     written(&out);
   });
@@ -368,12 +376,12 @@ PyObject* verify_drafts(PyObject*, PyObject* const* a, Py_ssize_t n_args) {
     c.device = gpu;
     if (k > 0 && (a[1] == Py_None || a[2] == Py_None)) throw Bad{"drafts need their tokens and random numbers"};
     if (a[3] == Py_None) throw Bad{"u_sample is needed"};
+    void* stream = stream_of(a[13], gpu);
     size_t need = 0;
     if (a[12] == Py_None) checked(bound.verify_workspace(&c, &need));
     const Workspace ws(a[12], gpu, a[13], need);
     c.workspace = ws.at;
     c.workspace_bytes = ws.bytes;
-    void* stream = stream_of(a[13], gpu);
     launch([&] { return bound.verify_drafts(&c, stream); });
     for (const int i : {5, 6, 11}) written(tensor("output", a[i]));
   });

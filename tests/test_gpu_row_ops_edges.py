@@ -268,3 +268,20 @@ def test_a_device_that_is_not_there_runs_nothing():
         assert torch.cuda.current_device() == 0
     torch.cuda.synchronize()
     assert bool((out == 7).all()) and bool((acc == 7).all()) and bool((tok == 7).all())
+
+
+def test_a_stream_of_another_gpu_is_refused():
+    from types import SimpleNamespace
+    x, out = torch.ones(2, 1, 64, device="cuda"), torch.full((2, 1, 64), 7.0, device="cuda")
+    here = torch.cuda.current_stream()
+    for stream, fine in ((SimpleNamespace(cuda_stream=here.cuda_stream, device_index=1), False), (here, True),
+                         (SimpleNamespace(cuda_stream=here.cuda_stream, device_index=0), True),
+                         (SimpleNamespace(cuda_stream=here.cuda_stream), True)):
+        out.fill_(7.0)
+        if fine:
+            spanq.qk_norm_rope(x, None, None, None, None, 0.0, out, None, None, stream=stream)
+        else:
+            with pytest.raises(spanq.SpanError) as e:
+                spanq.qk_norm_rope(x, None, None, None, None, 0.0, out, None, None, stream=stream)
+            assert e.value.code == -1
+        assert bool((out == (1.0 if fine else 7.0)).all())

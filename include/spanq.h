@@ -469,8 +469,8 @@ int span_model_set_adapters(span_model* model, const span_model_adapters* adapte
 
 /* The adapter of each of the plan's queries (host [n_queries], below 0: none; NULL: none at
  * all) in the span_model_* calls on it from here on, which return SPAN_EINVAL for an id that the model does
- * not have.  Set it before span_model_forward and leave it: the cross segment's keys and
- * values are the adapter's. */
+ * not have, or if queries of different adapters share cross rows.  Set it before
+ * span_model_forward and leave it: the cross segment's keys and values are the adapter's. */
 int span_plan_set_adapters(span_plan_t* plan, const int32_t* adapters);
 
 /* Run the rows a plan computes (span_plan_rows: new prefix/fragment tokens, then

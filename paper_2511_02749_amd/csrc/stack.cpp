@@ -747,7 +747,9 @@ int forward(span_model* m, span_plan_t* plan, const int32_t* row_tokens, int64_t
     plan_cross_spans(plan, &row0, &n);
     std::unordered_map<int64_t, int32_t> id_of;
     for (int qi = 0; qi < nq; ++qi)
-      for (int32_t j = 0; j < n[qi]; ++j) id_of[row0[qi] + j] = adapters[qi];
+      for (int32_t j = 0; j < n[qi]; ++j)
+        if (id_of.emplace(row0[qi] + j, adapters[qi]).first->second != adapters[qi])
+          return report(SPAN_EINVAL, "span_model_forward: queries with different adapters share cross rows");
     for (int64_t i = n_pre; i < T; ++i) {
       const auto it = id_of.find(h_rows[i]);
       h_ids[i - n_pre] = it != id_of.end() ? it->second : -1;

@@ -127,7 +127,20 @@ int main() {
     CHECK(last.pages[0].size() == (13 + 6 + 15) / 16 && last.pages[1].size() == 1);
     CHECK(span_plan_destroy(plan) == SPAN_OK);
   }
-  CHECK(span_model_destroy(model) == SPAN_OK);
+  span_model* shared = model;
+
+  // queries that share their cross rows have one activation for both: one adapter too
+  q[1].cross = q[0].cross;
+  for (int other : {-1, 1}) {
+    span_plan_t* plan = nullptr;
+    const int32_t both[2] = {1, other};
+    CHECK(span_plan(pool, q, 2, nullptr, &plan) == SPAN_OK && span_plan_set_adapters(plan, both) == SPAN_OK);
+    int32_t first[2];
+    CHECK(span_model_forward(shared, plan, tok.data(), 64, kLayers, nullptr, nullptr, first, nullptr) ==
+          (other == 1 ? SPAN_OK : SPAN_EINVAL));
+    CHECK(span_plan_destroy(plan) == SPAN_OK);
+  }
+  CHECK(span_model_destroy(shared) == SPAN_OK);
 
   // products wider than the operator takes are refused when they are given, not in the middle of a forward
   mc.ffn = (1 << 19) + 8;

@@ -22,6 +22,9 @@
 //
 // Bound: HBM (x, base and out for many rows, A and B for few); 2 R (K P + N) operations a row.
 // Decode steps are bound by the latency of their two launches and the loads in a row inside them.
+//
+// Times of calls are of captured ones, one after another over three sets of inputs; a kernel's alone is its
+// median in a trace of such calls.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -40,19 +43,19 @@ using mfma::pack_bf16x2;
 constexpr int kTile = 16;      // rows of a group, ranks of a block
 constexpr int kParts = 3;      // bf16 numbers that hold a value of H: high, middle, low
 constexpr int kFewRows = 256;  // at most, of the few-row form (few_rows)
-// Work-groups over K at most.  Few rows, 16 for 8: 48 rows of K 14336 15.5 -> 14.7 us, but 200 rows of
-// rank 128, whose partials are many, 35.7 -> 42.9.
+// Work-groups over K at most.  Few rows, 16 for 8: 48 rows of K 14336 18.3 -> 18.1 us, but 200 rows of
+// rank 128, whose partials are many, 33.3 -> 34.1.
 constexpr int kFewSlices = 8;
 constexpr int kManySlices = 16;
 constexpr int kXcds = 8;
-// Work-groups to which the adapters of a tile are dealt (in shrink, 2048 rows in four segments: 16.0
-// us with one, 12.9 with four; with eight, which are mostly empty, 1000 rows 23.4 -> 25.4 in all).
+// Work-groups to which the adapters of a tile are dealt (2048 rows of 28672 columns in four segments: 76.2
+// us with one, 73.4 with four; with eight, which are mostly empty, 1000 rows of 4096 columns 25.2 -> 28.1).
 constexpr int kManyGroups = 4;
 constexpr int kManyTiles = 4;  // 16-row tiles of a many-row work-group
 
 // Shrink work-groups: waves (each with its own part of K), 16-row and 16-column tiles of H,
 // and products of 32 values whose loads are in flight together (few rows: 16 KB a wave; with four
-// waves and half the loads 48 rows of K 14336 take 19.5 us for 19).
+// waves and half the loads 200 rows of rank 128 take 37.0 us for 33.3, 48 rows of K 14336 the same 18.2).
 struct FewShrink {
   static constexpr int kWaves = 2, kRows = 1, kCols = 1, kSteps = 8;
 };
@@ -252,8 +255,8 @@ __global__ __launch_bounds__(kOrderThreads) void adapter_order_kernel(const Shap
 }
 
 // H of one group (few) or of a tile of 64 ordered rows: one slice of K, C::kCols column tiles.
-// 64 rows of 64 adapters, K 4096, rank 16 (8.4 MB of A): 5.2 us; 48 rows of 12, K 14336, rank 64 (22
-// MB): 12 us, four rounds of loads one after another.  2048 rows, K 4096, 64 columns of H: 12.4 us.
+// 64 rows of 64 adapters, K 4096, rank 16 (8.4 MB of A): 5.0 us; 48 rows of 12, K 14336, rank 64 (22
+// MB): 11.7 us, four rounds of loads one after another.  2048 rows, K 4096, 64 columns of H: 12.0 us.
 template <bool kFew, class C>
 __global__ __launch_bounds__(64 * C::kWaves) void adapter_shrink_kernel(const Shape s) {
   __shared__ float4 red[C::kWaves][C::kCols][16 * C::kRows][4];
@@ -412,7 +415,7 @@ struct Cols {
 // J tiles of 16 columns: column m of tile j is column J m + j of the wave's, so that a lane's
 // results are J columns that follow one another.
 // kStream: base and out pass the caches by (a call of many rows reads and writes each of
-// their lines once: 2048 rows of 28672 columns 79 -> 74 us).
+// their lines once: 2048 rows of 28672 columns 74.3 -> 71.7 us, of 6144 at rank 128 68.4 -> 69.5).
 template <int J, bool kStream>
 struct Out {
   typedef uint32_t Vec __attribute__((ext_vector_type(J / 2)));
@@ -510,7 +513,9 @@ unsigned col_blocks(const Shape& s) {
 // One group of few rows, or a tile of 16 ordered rows of a call that has too few for runs: 64
 // columns a wave.  The slices' partials are added up on the way.  A tile's adapters are dealt to
 // kManyGroups work-groups, as in shrink.  64 rows of 64 adapters, 4096 columns, rank 16 (8.4 MB of
-// B): 7.5 us; 777 ordered rows of 2048 columns: 6.4.
+// B): 7.6 us; 777 ordered rows of 2048 columns: 7.0.
+// Waves a SIMD: five for few rows, three for a tile, which bounds the registers to 96 and 168; for `wild` the compiler
+// would take more (one row 7.4 us for 7.1).
 constexpr int kTileJ = 4;
 template <bool kFew>
 __global__ __launch_bounds__(64 * kExpandWaves, kFew ? 5 : 3) void adapter_expand_tile_kernel(const Shape s) {
@@ -626,17 +631,17 @@ __global__ __launch_bounds__(64 * kExpandWaves, kFew ? 5 : 3) void adapter_expan
 }
 
 // Many rows: 64 columns a wave, a run of tiles of 16 rows one after another.  The run's H lies in
-// LDS, which the four waves read instead of each fetching it (three parts of H from memory: 2048 rows of 28672
-// columns 64 us, from LDS 57); the next tile's base is on its way while a tile is worked, and the weights of
-// all kKept blocks of ranks stay in registers while the adapter stays (2048 rows of 6144 columns, rank 128: 67 us
-// in all).  2048 rows of 28672 columns, rank 32, move 235 MB in 57 us, 4.1 TB/s; were the
+// LDS, which the four waves read instead of each fetching it (2048 rows of 28672 columns: 7 us more with its three
+// parts from memory); the next tile's base is on its way while a tile is worked, and the weights of
+// all kKept blocks of ranks stay in registers while the adapter stays (2048 rows of 6144 columns, rank 128: 69.5 us
+// in all).  2048 rows of 28672 columns, rank 32, move 235 MB in 55 us, 4.3 TB/s; were the
 // weights asked for only once the rank is known, 6 us more.  Short runs (kShortRun) have a form with room for no
-// more in LDS and registers: 300 rows of 8200 columns, rank 128, 37.6 us for 40.6.
+// more in LDS and registers: 300 rows of 8200 columns, rank 128, 38.1 us for 40.8.
 constexpr int kManyJ = 4;
 constexpr int kManyRun = 8;  // at most
 constexpr int kShortRun = 2;
-// (Two blocks kept: three waves a SIMD, at most 168 registers. `wild` would have the compiler take 176: 79 us for 75 for
-// 2048 rows of 28672 columns in all.)
+// (Two blocks kept: three waves a SIMD, at most 168 registers.  For `wild` the compiler would take 176: 2048 rows of
+// 28672 columns 79 us for 74 in all, not captured.)
 template <int kKept, int kRun>
 __global__ __launch_bounds__(64 * kExpandWaves, kKept == 2 ? 3 : 1) void adapter_expand_many_kernel(const Shape s) {
   constexpr int J = kManyJ;
@@ -781,18 +786,21 @@ unsigned h_groups(const Shape& s) {
 }
 
 // Rows up to which the few-row form serves.  It reads B again for each 16 rows of an adapter,
-// the many-row form orders the rows first and gains by long runs.  Captured calls of K 4096, few /
-// many in us, 1 adapter and 32 mixed ones:
-//   N 4096, rank 16:   130 rows 15.0 / 13.2, 10.0 / 27.6   256 rows 20.2 / 13.3, 13.0 / 18.4
-//   N 28672, rank 32:   96 rows 25.5 / 19.0, 39.3 / 53.1   192 rows 42.7 / 25.0, 54.1 / 47.1
+// the many-row form orders the rows first and gains by long runs.  K 4096, few / many in us, 1 adapter and 32 mixed
+// ones:
+//   N 4096, rank 16:   130 rows 16.3 / 13.4, 12.5 / 27.2   256 rows 20.2 / 13.8, 14.2 / 24.9
+//   N 8192, rank 32:   192 rows 25.9 / 16.0, 21.1 / 34.1   N 12288: 29.8 / 18.4, 25.9 / 36.2
+//   N 28672, rank 32:   96 rows 24.2 / 18.5, 36.8 / 50.4   192 rows 42.3 / 24.7, 47.0 / 48.9
+// Mixed adapters lose more by the other form than one adapter does up to these rows, and a call does not say how many of
+// its adapters occur; one adapter's rows by themselves, up to here, would be better off with the many-row form.
 constexpr int kNarrow = 8192;
 int few_rows(const Shape& s) { return s.N <= kNarrow ? kFewRows : kFewRows / 2; }
 
 // Many rows, but too few for runs: their expand adds the slices' partials up itself, up to so
 // many blocks of 16 ranks of them for a row, a launch less; every work-group across the columns does
 // it again.  Itself / by a launch, us:
-//   N 4096, rank 16:   257 rows 13.7 / 16.2, 384 rows of 32 mixed adapters 20.8 / 23.6
-//   N 28672, rank 32:  130 rows 24.5 / 21.5, 32 mixed adapters 68.7 / 55.4
+//   N 4096, rank 16:   257 rows 14.0 / 16.4, 384 rows of 32 mixed adapters 25.6 / 26.9
+//   N 28672, rank 32:  130 rows 24.6 / 22.3, 32 mixed adapters 62.4 / 52.2
 constexpr int kTilePartials = 32;
 
 // `rows` rows of the call from `first` on; *bytes: of the workspace they need.
@@ -818,8 +826,8 @@ Shape shape_of(const span_adapter_call& c, int64_t first, int64_t rows, size_t* 
   s.rank_blocks = (s.R + 15) / 16;
   s.h_cols = 16 * s.n_parts * s.rank_blocks;
   // K slices: enough work-groups for the chip, and for many rows a multiple of the XCDs' number where K
-  // allows it and partials are not too many (10000 rows: K 4096, 16 columns of H 88 us with eight, 102
-  // with one; K 2048, 128 columns 122 and 95)
+  // allows it and partials are not too many (10000 rows: K 4096, 16 columns of H 90 us with eight, 107
+  // with one; K 2048, 128 columns 160 and 131)
   const bool few = rows <= few_rows(s);
   const int unit = 32 * (few ? FewShrink::kSteps * FewShrink::kWaves : ManyShrink::kSteps * ManyShrink::kWaves);
   const int64_t most = (s.K + unit - 1) / unit;

@@ -636,7 +636,8 @@ __global__ __launch_bounds__(64 * kExpandWaves, kFew ? 5 : 3) void adapter_expan
 // all kKept blocks of ranks stay in registers while the adapter stays (2048 rows of 6144 columns, rank 128: 69.5 us
 // in all).  2048 rows of 28672 columns, rank 32, move 235 MB in 55 us, 4.3 TB/s; were the
 // weights asked for only once the rank is known, 6 us more.  Short runs (kShortRun) have a form with room for no
-// more in LDS and registers: 300 rows of 8200 columns, rank 128, 38.1 us for 40.8.
+// more in LDS and registers (300 rows of 8200 columns, rank 128, 38.3 us for 40.8), and of small ranks take H with
+// the base, from memory (192 rows of 28672 columns, 32 mixed adapters, 48.7 us for 50.5; rank 128 39.2 for 38.3).
 constexpr int kManyJ = 4;
 constexpr int kManyRun = 8;  // at most
 constexpr int kShortRun = 2;
@@ -652,7 +653,8 @@ __global__ __launch_bounds__(64 * kExpandWaves, kKept == 2 ? 3 : 1) void adapter
   constexpr int kVecs = 2 * kParts;            // of 16 bytes in a block of ranks
   constexpr int kRowVecs = kVecs * kKept + 1;  // (16 rows' reads fall on different banks)
   __shared__ int list[16 * kRun];  // rows of the call
-  __shared__ uint4 hs[16 * kRun * kRowVecs];
+  constexpr bool kLds = kRun > kShortRun || kKept > 2;
+  __shared__ uint4 hs[kLds ? 16 * kRun * kRowVecs : 1];
   const Cols cols = cols_of<J>(s, blockIdx.x, wave_id());
   const bool in_place = s.base == s.out && s.base_stride == s.out_stride;
   const bool has_col = cols.n0 + J * m < cols.width;
@@ -665,13 +667,13 @@ __global__ __launch_bounds__(64 * kExpandWaves, kKept == 2 ? 3 : 1) void adapter
     rows[i] = at.x;
     ids[i] = at.y;
   }
-  // The run's H, which all waves read, in LDS; asked for together with the rows.  Rows past the last and
-  // blocks past the last hold some finite part: no result of theirs is used, or their weights are zero.
+  // The run's H, which all waves read, in LDS; asked for together with the rows.  Rows past the last and blocks
+  // past the last hold parts of the last: no result of theirs is used, or they meet weights of zero.
   const uint4* h0 = reinterpret_cast<const uint4*>(s.h + kParts * (row0 * s.h_cols + cols.part * s.rank_blocks * 16));
   constexpr int kAll = kVecs * kKept * 16 * kRun, kEach = (kAll + kThreads - 1) / kThreads;
   uint4 hv[kEach];
 #pragma unroll
-  for (int u = 0; u < kEach; ++u) {
+  for (int u = 0; u < kEach && kLds; ++u) {
     const int e = u * kThreads + threadIdx.x, r = min(e / (kVecs * kKept), n_rows - 1);
     const int v = min(e % (kVecs * kKept), kVecs * s.rank_blocks - 1);
     hv[u] = h0[static_cast<uint32_t>(r * (kVecs * s.h_cols / 16) + v)];
@@ -680,20 +682,30 @@ __global__ __launch_bounds__(64 * kExpandWaves, kKept == 2 ? 3 : 1) void adapter
   for (int i = 0; i < (16 * kRun + 63) / 64; ++i)
     if (wave_id() == 0 && 64 * i + lane < n_rows) list[64 * i + lane] = rows[i];
 #pragma unroll
-  for (int u = 0; u < kEach; ++u) {
+  for (int u = 0; u < kEach && kLds; ++u) {
     const int e = u * kThreads + threadIdx.x;
     if (kAll % kThreads == 0 || e < kAll) hs[e / (kVecs * kKept) * kRowVecs + e % (kVecs * kKept)] = hv[u];
   }
   __syncthreads();
   if (cols.n0 >= cols.width) return;
   // vector `at` of block rb of row r of H
-  auto load_h = [&](int r, int rb, int at) { return hs[r * kRowVecs + kVecs * rb + at]; };
+  auto load_h = [&](int r, int rb, int at) {
+    if constexpr (kLds) return hs[r * kRowVecs + kVecs * rb + at];
+    return h0[static_cast<uint32_t>(min(r, n_rows - 1) * (kVecs * s.h_cols / 16) + kVecs * min(rb, s.rank_blocks - 1) + at)];
+  };
   const bf16_t* base = s.base + cols.col0;
   bf16_t* out = s.out + cols.col0;
   struct Ahead {
     typename O::Vec base[4];
+    uint4 h[kLds ? 1 : kKept], low[kLds ? 1 : kKept / 2];
   };
   auto fetch = [&](int t, Ahead& a) {
+    if constexpr (!kLds) {
+#pragma unroll
+      for (int k = 0; k < kKept; ++k) a.h[k] = load_h(16 * t + m, k, g);
+#pragma unroll
+      for (int k = 0; k < kKept; k += 2) a.low[k / 2] = load_h(16 * t + m, k + (g >> 1), 4 + (g & 1));
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) a.base[i] = O::base(base, s.base_stride, cols, list[min(16 * t + 4 * g + i, n_rows - 1)], m);
   };
@@ -718,16 +730,17 @@ __global__ __launch_bounds__(64 * kExpandWaves, kKept == 2 ? 3 : 1) void adapter
   };
   // Of H, a lane's ranks 8 (g & 1) .. of a block: high (g < 2) or middle parts; of two blocks, the
   // first's (g < 2) or the second's low parts.
-  auto multiply = [&](int t, f32x4_t (&acc)[J]) {
+  auto multiply = [&](int t, const Ahead& a, f32x4_t (&acc)[J]) {
+    auto h_of = [&](int k) { return kLds ? load_h(16 * t + m, k, g) : a.h[kLds ? 0 : k]; };
 #pragma unroll
     for (int k = 0; k < kKept; k += 2) {
       if (16 * k >= rank) break;
       uint4 w[J];  // (past the rank they are zero, and low parts are finite)
 #pragma unroll
       for (int j = 0; j < J; ++j) w[j] = g < 2 ? wv[k][j] : wv[k + 1][j];
-      multiply_h(load_h(16 * t + m, k + (g >> 1), 4 + (g & 1)), w, acc);
-      multiply_h(load_h(16 * t + m, k, g), wv[k], acc);
-      if (16 * k + 16 < rank) multiply_h(load_h(16 * t + m, k + 1, g), wv[k + 1], acc);
+      multiply_h(kLds ? load_h(16 * t + m, k + (g >> 1), 4 + (g & 1)) : a.low[kLds ? 0 : k / 2], w, acc);
+      multiply_h(h_of(k), wv[k], acc);
+      if (16 * k + 16 < rank) multiply_h(h_of(k + 1), wv[k + 1], acc);
     }
     if (__builtin_expect(any_wild(acc), 0))
       O::template wild<true>(s, cols, kept, rank, m, g, [&](int rb, int at) { return load_h(16 * t + m, rb, at); }, acc);
@@ -746,7 +759,7 @@ __global__ __launch_bounds__(64 * kExpandWaves, kKept == 2 ? 3 : 1) void adapter
       now = ahead;
       fetch(t + 1, ahead);  // (of the last tile: the last row again)
       f32x4_t acc[J] = {};
-      multiply(t, acc);
+      multiply(t, now, acc);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         O::store(out, s.out_stride, cols, list[16 * t + 4 * g + i], m, O::add(now.base[i], acc, i, scale));
@@ -762,7 +775,7 @@ __global__ __launch_bounds__(64 * kExpandWaves, kKept == 2 ? 3 : 1) void adapter
       f32x4_t acc[J] = {};
       if (aid >= 0) {
         if (aid != kept) keep(aid);
-        multiply(t, acc);
+        multiply(t, now, acc);
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i)

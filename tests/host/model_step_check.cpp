@@ -108,7 +108,7 @@ int main() {
     failed += each_failure(pool, plan, allocations, [&] {
       return span_model_forward(model, plan, tok.data(), 64, kLayers, nullptr, nullptr, first, nullptr);
     }, [] {});
-    for (int round = 0; round < 3; ++round) {
+    for (int again = 0; again < 3; ++again) {
       failed += each_failure(pool, plan, allocations, [&] { return span_model_decode(model, plan, next, nullptr, first, nullptr); },
                              [&] {
                                const int32_t back[2] = {1, 1};

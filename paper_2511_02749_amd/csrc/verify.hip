@@ -378,13 +378,19 @@ __device__ __forceinline__ int accept(const Args& a, int q, const Request& r, Ve
   return n;
 }
 
-__device__ __forceinline__ double inverse(double s) { return s > 0.0 ? 1.0 / s : 0.0; }
+// A row's sum of weights and its inverse, 0 and 0 if there are none.
+struct Whole {
+  double sum, inverse;
+};
+__device__ __forceinline__ Whole whole_of(double s) { return s > 0.0 ? Whole{s, 1.0 / s} : Whole{0.0, 0.0}; }
 
-// max(p - q, 0) of two weights and the inverses of their rows' sums, each product rounded: contracted
-// to an fma the difference of equal ones would be a rounding, not 0, and where p = q nothing may be left.
-__device__ __forceinline__ double residue(double p, double ps, double q, double qs) {
-#pragma clang fp contract(off)
-  const double a = p * ps, b = q * qs;
+// max(p - q, 0) of two weights and their rows' sums.  Both quotients are rounded as divisions are, and before the
+// difference: otherwise that of equal ones, or of two that are all of their rows, would be a rounding, not 0, and
+// where p = q nothing may be left.
+__device__ __forceinline__ double residue(double p, const Whole& ps, double q, const Whole& qs) {
+  double a = p * ps.inverse, b = q * qs.inverse;
+  a = fma(fma(-ps.sum, a, p), ps.inverse, a);
+  b = fma(fma(-qs.sum, b, q), qs.inverse, b);
   return fmax(a - b, 0.0);
 }
 
@@ -393,11 +399,11 @@ struct Left {
   const float* x;
   const float* y;  // the draft's logits, or null
   Scale p, q;
-  double ps, qs;  // 1 / sums
+  Whole ps, qs;
   int one_hot;    // the token taken out of p where the draft has no distribution, -1: none
   __device__ __forceinline__ double of(int i, float xi, float yi) const {
     if (y) return residue(weight(xi, p), ps, weight(yi, q), qs);
-    return i == one_hot ? 0.0 : weight(xi, p) * ps;
+    return i == one_hot ? 0.0 : weight(xi, p) * ps.inverse;
   }
 };
 
@@ -407,13 +413,13 @@ __device__ __forceinline__ Left left_of(const Args& a, int q, const Request& r, 
   Left l{};
   l.x = c.target_logits + (r.target_row + n) * c.target_stride;
   l.p = scale_of(v.p[n].max, r.c);
-  l.ps = inverse(v.p[n].sum);
+  l.ps = whole_of(v.p[n].sum);
   l.one_hot = -1;
   if (n < r.n_drafts && !plain) {
     if (c.draft_logits) {
       l.y = c.draft_logits + (r.draft_row + n) * c.draft_stride;
       l.q = scale_of(v.q[n].max, r.c);
-      l.qs = inverse(v.q[n].sum);
+      l.qs = whole_of(v.q[n].sum);
     } else {
       const int d = v.d[n];
       l.one_hot = d >= 0 && d < c.vocab ? d : -1;
@@ -503,8 +509,8 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(const Args a)
       auto chunk_sum = [&](int i) -> double {
         if (i >= a.chunks) return 0.0;
         if (l.y) return a.left[static_cast<int64_t>(q) * a.chunks + i];
-        if (l.one_hot >= 0 && l.one_hot / kChunk == i) return in_row(v.q[n], l.p) * l.ps;
-        return (i < 64 ? s_chunk[n][i] : in_row(st[i], l.p)) * l.ps;
+        if (l.one_hot >= 0 && l.one_hot / kChunk == i) return in_row(v.q[n], l.p) * l.ps.inverse;
+        return (i < 64 ? s_chunk[n][i] : in_row(st[i], l.p)) * l.ps.inverse;
       };
       const double own = chunk_sum(lane);  // all of them up to 64 chunks
       double total = 0.0;

@@ -187,6 +187,25 @@ def test_rotations_by_the_angle_and_not_by_a_float_next_to_it(dim, theta):
     assert bool((err <= bound).all())
 
 
+@pytest.mark.parametrize("V", [300, 5003, 40000])
+def test_a_token_that_is_all_of_both_rows_leaves_nothing(V):
+    """Target and draft with all their weight, as far as 64 bits tell, on one token: p = q = 1 there, so that
+    after a refused draft only what p has over q of the others is left, however little."""
+    n, k = 40, 1
+    target, draft, drafts, ua, us, heat = _logits(n, k, V, V, True)
+    g, heat = _gen(V), heat.clamp(min=0.2)
+    top = torch.randint(0, V, (n,), generator=g)
+    t, y = target.view(n, k + 1, V), draft.view(n, k, V)
+    gap = 60.0 * heat  # others: below e^-40 each, where a row's rounding is e^-37
+    for i in range(n):
+        t[i, :, top[i]], y[i, :, top[i]] = t[i].max() + gap[i], y[i].max() + gap[i] + 0.3
+    drafts = ((top + 1 + torch.randint(0, V - 1, (n,), generator=g)) % V).to(torch.int32)[:, None]
+    y[torch.arange(n), 0, drafts[:, 0].long()] += 5.0  # q(d) > p(d)
+    ua[:] = 1 - 2.0 ** -24
+    acc, tok, _ = _verify_and_check(target, draft, drafts, None, ua, us, heat, None, None, k, f"all of both rows, V {V}")
+    assert (acc == 0).all() and not (tok[:, 0] == top.numpy()).any()
+
+
 def test_logits_without_any_rows_are_not_logits_that_were_not_given():
     """Requests whose rows lie outside logits of no rows at all: -1, as outside any others; requests without drafts
     need no draft rows."""
